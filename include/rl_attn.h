@@ -69,7 +69,7 @@ extern "C" {
 
 /* RL_FP8_E4M3: one byte per element, the OCP 8-bit E4M3 format (exponent bias
  * 7, no infinities, 0x7F/0xFF are NaN, largest finite magnitude 448). */
-enum rl_dtype { RL_BF16 = 1, RL_F32 = 2, RL_I32 = 3, RL_FP8_E4M3 = 4 };
+enum rl_dtype { RL_BF16 = 1, RL_F32 = 2, RL_I32 = 3, RL_FP8_E4M3 = 4, RL_I64 = 5 };
 
 enum rl_status {
   RL_OK = 0,
@@ -253,6 +253,105 @@ int rl_attn_append_kv_fp8(const rl_tensor* k_new, const rl_tensor* v_new, const 
                           rl_tensor* v_pages, const rl_tensor* k_scale, const rl_tensor* v_scale,
                           void* stream);
 
+/* ---- a step's rows: where they go, their positions, their first attention ----
+ * An engine's step is rl_attn_map_slots, then per layer rl_attn_rope_append_kv
+ * and rl_attn_prefill (first turns), rl_attn_extend (later ones) or
+ * rl_attn_decode. */
+
+/* Slot maps (paper: every turn appends its suffix to cached context, section
+ * "Fast Agentic Rollout with SGLang"): from the lengths of a step's requests,
+ * their new block-table entries, the row bounds of the attention calls, and a
+ * slot and a position for each new row, on the device, so that a step needs
+ * no copy from the host.
+ *   kv_lens    [B] int32: tokens request b has cached (c_b)
+ *   new_lens   [B] int32: tokens the step adds (n_b >= 0)
+ *   free_pages [F] int32: ids of free pages, taken in order
+ *   free_used  [1] int32: how many of them earlier steps have taken
+ *   pos_delta  [B] int32, nullable: token t has position t + pos_delta[b]
+ *   page_size, num_pages: of the pool (page ids outside it are refused)
+ *   block_table [B, max_pages] int32: its entries for c_b cached tokens are
+ *              read, those of new pages are written, no other is touched
+ *   kv_lens_out [B], free_used_out [1] int32: c_b + n_b, and the entries now
+ *              taken; may be kv_lens and free_used themselves (a step in place),
+ *              else must not overlap them
+ *   qo_indptr  [B+1] int32: row bounds, qo_indptr[b+1] - qo_indptr[b] = n_b
+ *   slot_map   [T] int64, T >= sum of n_b: page * page_size + slot in the page
+ *              of each row; -1 in the rows behind the last request's
+ *   positions  [T] int32 (0 in the rows behind the last request's)
+ * Pages that are shared are full ones: a request's last partly filled page must
+ * be its own. A request with a negative length, or longer than its table, gets
+ * nothing (n_b counts as 0) and is reported by rl_attn_check_device_errors().
+ * Requests are served in order: from the first whose rows do not fit T or whose
+ * pages are more than the list has left on, none gets anything, which is
+ * reported too. A row whose page id (of the list or the table) is outside the
+ * pool gets slot -1 and is reported. One launch (two for more than 1024 rows
+ * in place); allocates nothing beyond the library's per-stream error word. */
+int rl_attn_map_slots(const rl_tensor* kv_lens, const rl_tensor* new_lens, const rl_tensor* free_pages,
+                      const rl_tensor* free_used, const rl_tensor* pos_delta, int64_t page_size, int64_t num_pages,
+                      rl_tensor* block_table, rl_tensor* kv_lens_out, rl_tensor* free_used_out, rl_tensor* qo_indptr,
+                      rl_tensor* slot_map, rl_tensor* positions, void* stream);
+
+/* Options of the rotary calls; NULL means all zeros. */
+typedef struct {
+  int32_t interleaved;   /* 0: dimension i turns with F + i; 1: 2i with 2i + 1 */
+  int32_t inverse;       /* rl_attn_rope: turn back (also the gradient)        */
+  int32_t reserved[6];   /* must be zero                                       */
+} rl_rope_opts;
+
+/* Rotary positions with one or several axes. For F frequencies the pair (x, y)
+ * number i of a row's first 2F dimensions becomes (x cos a - y sin a, y cos a +
+ * x sin a) with a = positions[axes[i], row] * inv_freq[i]; the other dimensions
+ * are copied. The angle is formed in 64 bits, the pair in 32, rounded once.
+ *   q          [T, Hq, 128] bf16
+ *   k          [T, Hkv, 128] bf16, nullable (then k_out is NULL too)
+ *   positions  [A, T] int32, any strides from 0 on (an expanded row serves all axes)
+ *   inv_freq   [F] f32, F a multiple of 8 in [8, 64]
+ *   axes       [F] int32: the axis (row of positions) of each frequency, e.g.
+ *              time, height and width in blocks or in turn; NULL for A = 1. An
+ *              axis outside [0, A) is clamped and reported.
+ *   q_out, k_out: as q and k, and may be q and k (the same view); they must not
+ *              overlap them otherwise */
+int rl_attn_rope(const rl_tensor* q, const rl_tensor* k, const rl_tensor* positions, const rl_tensor* inv_freq,
+                 const rl_tensor* axes, const rl_rope_opts* opts, rl_tensor* q_out, rl_tensor* k_out, void* stream);
+
+/* The same in one pass with the append of the rows to their pages:
+ *   v_new      [T, Hkv, 128] bf16
+ *   slot_map   [T] int64, as rl_attn_map_slots writes it. A row with a negative
+ *              slot is skipped: nothing is written for it, q_out and k_out
+ *              included. A slot past the pool's end is reported, and its row not
+ *              appended.
+ *   k_out      [T, Hkv, 128] bf16, nullable: the rotated keys as rows too, for
+ *              rl_attn_prefill
+ *   k_pages, v_pages [num_pages, P, Hkv, 128]: only the slots are written
+ * The FP8 call takes E4M3 pages and the scales of rl_attn_append_kv_fp8 and
+ * writes the codes nearest to the float32 quotient of the rotated float32 key
+ * (not rounded to bf16 first) or the value by its head's scale. Rows that map to
+ * one slot race. */
+int rl_attn_rope_append_kv(const rl_tensor* q, const rl_tensor* k_new, const rl_tensor* v_new,
+                           const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                           const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out, rl_tensor* k_out,
+                           rl_tensor* k_pages, rl_tensor* v_pages, void* stream);
+
+int rl_attn_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const rl_tensor* v_new,
+                               const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                               const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out,
+                               rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, const rl_tensor* k_scale,
+                               const rl_tensor* v_scale, void* stream);
+
+/* Causal attention over whole packed prompts (the first turn of a trajectory
+ * group, before there is a cache to extend): row i of prompt b attends to its
+ * rows 0 .. i, read from packed rows and not from pages.
+ *   q          [T, Hq, 128] bf16
+ *   k, v       [T, Hkv, 128] bf16 (row strides below 2^24 elements)
+ *   seq_indptr [B+1] int32: prompt b owns rows seq_indptr[b] .. seq_indptr[b+1]-1;
+ *              bounds that decrease or leave [0, T] are clamped and reported
+ *   out        [T, Hq, 128] bf16 (f32 also accepted); lse_out [T, Hq] f32,
+ *              nullable. Rows that no prompt owns are left as they were.
+ * A row's results depend on no row behind it, whatever that row holds (NaN and
+ * infinities included). */
+int rl_attn_prefill(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const rl_tensor* seq_indptr,
+                    float scale, rl_tensor* out, rl_tensor* lse_out, void* stream);
+
 /* Log-sum-exp merge of partial attention results over disjoint key ranges
  * (the split-KV combine, exposed for testing and for callers that split work
  * themselves):
@@ -301,12 +400,13 @@ size_t rl_attn_extend_workspace_size(int64_t batch, int64_t total_q, int64_t num
                                      int64_t num_kv_heads, int64_t max_pages, int64_t page_size);
 
 /* Kernel timing for benchmarks and profiling tools. While enabled, each
- * decode / extend / append call brackets its main kernel with a pair of HIP
+ * decode / extend / append / prefill / rotary call brackets its main kernel with a pair of HIP
  * events on the call's stream (the planner and combine kernels are outside
  * the pair). rl_attn_profile_read() waits for the recorded events and returns
  * the number of timed launches and their mean duration in milliseconds per
  * kind (kind 0 = decode attention kernel, 1 = extend attention kernel, 2 =
- * KV append kernel; a deterministic decode counts as kind 0), then forgets
+ * KV append kernel, 3 = prefill kernel, 4 = rotary kernel, alone or with its
+ * append; a deterministic decode counts as kind 0), then forgets
  * them. Disabled by default; enabling costs two event records per call. */
 int rl_attn_profile_enable(int on);
 int rl_attn_profile_read(int kind, int* launches, double* mean_ms);

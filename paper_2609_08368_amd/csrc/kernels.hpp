@@ -15,6 +15,10 @@ enum DeviceError : int {
   kErrScale = 16,    // an FP8 dequantisation scale that is not positive and finite
   kErrCapacity = 32, // the work of a call exceeded its workspace's capacity (affected
                      // outputs are NaN or left unwritten; the host sizing rules out this case)
+  kErrRows = 64,     // a request's rows end past the slot map
+  kErrPool = 128,    // the list of free pages is exhausted
+  kErrSlot = 256,    // a slot at or past the end of the page pool
+  kErrAxis = 512,    // an axis of a frequency outside the rows of positions (clamped)
 };
 
 // Slot markers of a decode piece: its result goes straight to out/lse, or
@@ -236,6 +240,76 @@ struct AppendArgs {
   int* err;
 };
 
+// Slot maps: pages, slots and positions of a step's rows from the lengths of its requests.
+struct MapArgs {
+  const int* kv_lens;     // [B] tokens cached before the step
+  const int* new_lens;    // [B] tokens it adds
+  const int* free_pages;  // [n_free] ids, the first *free_used taken
+  const int* free_used;
+  const int* delta;       // nullable: [B] position of token t is t + delta[b]
+  int64_t kv_s, new_s, free_s, delta_s;
+  int* bt;                // [B, max_pages], written where pages are taken
+  int64_t bt_sb, bt_sj;
+  int* kv_out;            // [B] (may be kv_lens)
+  int* used_out;          // (may be free_used)
+  int* indptr;            // [B + 1]
+  int64_t* slots;         // [rows]
+  int* pos;               // [rows]
+  int64_t kv_out_s, indptr_s, slots_s, pos_s;
+  int B, rows, n_free, num_pages, page_size, log2_page, max_pages;
+  int rows_block;         // rows of a workgroup
+  int late;               // kv_out and used_out are left to a second launch (they are read by every workgroup)
+  int* err;
+};
+
+// Rotary positions of query and key rows, alone or with the append of the key and value rows.
+struct RopeArgs {
+  const void* q;          // [rows, Hq, 128] bf16
+  const void* k;          // [rows, Hkv, 128] bf16 (Hkv = 0: none)
+  const void* v;          // append: [rows, Hkv, 128] bf16
+  int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh;
+  const int* pos;         // [n_axes, rows]
+  int64_t pos_sa, pos_st;
+  const float* inv_freq;  // [freqs]
+  const int* axes;        // nullable: [freqs] row of pos that turns a frequency
+  int64_t freq_s, axes_s;
+  void* q_out;
+  void* k_out;            // nullable with an append
+  int64_t qo_st, qo_sh, ko_st, ko_sh;
+  const int64_t* slots;   // append: [rows] slot of each row in the pages, negative: the row is not touched
+  int64_t slots_s;
+  void* k_pages;          // [num_pages, P, Hkv, 128] bf16 or E4M3
+  void* v_pages;
+  int64_t kp_sp, kp_ss, kp_sh, vp_sp, vp_ss, vp_sh;
+  const float* k_scale;   // FP8 pages: [Hkv]
+  const float* v_scale;
+  int64_t ks_s, vs_s;
+  int rows, Hq, Hkv, freqs, n_axes, interleaved, inverse;
+  int num_pages, page_size, log2_page;
+  int* err;
+};
+
+// Causal attention over whole packed prompts.
+struct PrefillArgs {
+  const void* q;          // [rows, Hq, 128] bf16
+  const void* k;          // [rows, Hkv, 128] bf16
+  const void* v;
+  int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh;
+  const int* indptr;      // [B + 1]
+  int64_t indptr_s;
+  int B, rows, Hq, Hkv, R;
+  int rows_head;          // query heads per tile
+  int tile_tokens;        // prompt tokens per tile
+  int head_blocks;        // ceil(R / rows_head)
+  float scale;
+  void* out;
+  int out_f32;
+  int64_t out_st, out_sh;
+  float* lse;
+  int64_t lse_st, lse_sh;
+  int* err;
+};
+
 // Optional events around the main attention kernel (benchmark timing).
 struct KernelTimer {
   hipEvent_t start = nullptr, stop = nullptr;
@@ -269,5 +343,8 @@ int decode_workers_per_cu(int R, int Hkv, int item_waves, bool fp8, int n_tok, i
 hipError_t launch_extend(const ExtendArgs& a, hipStream_t stream, KernelTimer* timer);
 hipError_t launch_merge(const MergeArgs& a, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream, KernelTimer* timer);
+hipError_t launch_map(const MapArgs& a, hipStream_t stream);
+hipError_t launch_rope(const RopeArgs& a, hipStream_t stream, KernelTimer* timer);
+hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream, KernelTimer* timer);
 
 }  // namespace rl

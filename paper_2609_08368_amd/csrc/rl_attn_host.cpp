@@ -96,6 +96,7 @@ const char* dtype_name(int d) {
     case RL_F32: return "f32";
     case RL_I32: return "int32";
     case RL_FP8_E4M3: return "fp8_e4m3";
+    case RL_I64: return "int64";
     default: return "unknown";
   }
 }
@@ -301,7 +302,7 @@ int get_ws(hipStream_t st, size_t need, size_t want, bool need_stash, int cus, b
 struct Profiler {
   std::mutex mu;
   bool on = false;
-  std::vector<rl::KernelTimer> pending[3];   // decode, extend, append
+  std::vector<rl::KernelTimer> pending[5];   // decode, extend, append, prefill, rotary rows
 };
 
 Profiler& prof() {
@@ -990,6 +991,310 @@ int append_impl(const rl_tensor* k_new, const rl_tensor* v_new, const rl_tensor*
   return RL_OK;
 }
 
+// ----------------------------------------------------------------- slot maps
+// A vector of the given length; its stride may be anything from 0 (read only) or 1 on.
+int check_vector(const rl_tensor* t, const char* name, int dtype, int64_t len, bool written) {
+  RL_TRY(check_view(t, name, 1));
+  RL_TRY(check_dtype(t, name, dtype));
+  if (t->shape[0] != len)
+    return fail(RL_ERR_SHAPE, "%s must have %lld entries (got %lld)", name, (long long)len, (long long)t->shape[0]);
+  if (t->strides[0] < 0 || t->strides[0] > INT32_MAX || (written && len > 1 && t->strides[0] < 1))
+    return fail(RL_ERR_UNSUPPORTED, "%s: stride must be in [%d, 2^31)", name, written ? 1 : 0);
+  return check_data(t, name);
+}
+
+int map_impl(const rl_tensor* kv_lens, const rl_tensor* new_lens, const rl_tensor* free_pages,
+             const rl_tensor* free_used, const rl_tensor* pos_delta, int64_t page_size, int64_t num_pages,
+             rl_tensor* block_table, rl_tensor* kv_lens_out, rl_tensor* free_used_out, rl_tensor* qo_indptr,
+             rl_tensor* slot_map, rl_tensor* positions, void* stream) {
+  RL_TRY(check_view(kv_lens, "kv_lens", 1));
+  const int64_t B = kv_lens->shape[0];
+  if (B > (1 << 22)) return fail(RL_ERR_UNSUPPORTED, "batch too large");
+  RL_TRY(check_vector(kv_lens, "kv_lens", RL_I32, B, false));
+  RL_TRY(check_vector(new_lens, "new_lens", RL_I32, B, false));
+  RL_TRY(check_view(free_pages, "free_pages", 1));
+  RL_TRY(check_vector(free_pages, "free_pages", RL_I32, free_pages->shape[0], false));
+  RL_TRY(check_vector(free_used, "free_used", RL_I32, 1, false));
+  if (pos_delta) RL_TRY(check_vector(pos_delta, "pos_delta", RL_I32, B, false));
+  if (page_size < 8 || page_size > 128 || (page_size & (page_size - 1)) != 0)
+    return fail(RL_ERR_UNSUPPORTED, "page size must be a power of two in [8, 128] (got %lld)", (long long)page_size);
+  if (num_pages < 0) return fail(RL_ERR_INVALID_ARG, "num_pages is negative");
+  RL_TRY(check_view(block_table, "block_table", 2));
+  RL_TRY(check_dtype(block_table, "block_table", RL_I32));
+  if (block_table->shape[0] != B)
+    return fail(RL_ERR_SHAPE, "block_table.shape[0] (%lld) != batch (%lld)", (long long)block_table->shape[0],
+                (long long)B);
+  // (the bounds of the attention calls that read the table)
+  const int64_t max_pages = block_table->shape[1], lim24 = (int64_t)1 << 24;
+  if (num_pages > INT32_MAX || free_pages->shape[0] > INT32_MAX || max_pages >= lim24 ||
+      max_pages * page_size > INT32_MAX)
+    return fail(RL_ERR_UNSUPPORTED, "page pool or block table too large for 32-bit token indices");
+  if (block_table->strides[0] < 0 || block_table->strides[1] < 0 || block_table->strides[1] >= lim24 ||
+      (B > 0 && max_pages > 1 && block_table->strides[1] < 1) || (B > 1 && max_pages > 0 && block_table->strides[0] < 1))
+    return fail(RL_ERR_UNSUPPORTED, "block_table: strides must be positive, the column stride below 2^24");
+  RL_TRY(check_data(block_table, "block_table"));
+  RL_TRY(check_vector(kv_lens_out, "kv_lens_out", RL_I32, B, true));
+  RL_TRY(check_vector(free_used_out, "free_used_out", RL_I32, 1, true));
+  RL_TRY(check_vector(qo_indptr, "qo_indptr", RL_I32, B + 1, true));
+  RL_TRY(check_view(slot_map, "slot_map", 1));
+  const int64_t rows = slot_map->shape[0];
+  if (rows > INT32_MAX / 2) return fail(RL_ERR_UNSUPPORTED, "slot map too long");
+  RL_TRY(check_vector(slot_map, "slot_map", RL_I64, rows, true));
+  RL_TRY(check_vector(positions, "positions", RL_I32, rows, true));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
+  rl::MapArgs a{};
+  a.kv_lens = static_cast<const int*>(kv_lens->data);
+  a.new_lens = static_cast<const int*>(new_lens->data);
+  a.free_pages = static_cast<const int*>(free_pages->data);
+  a.free_used = static_cast<const int*>(free_used->data);
+  a.delta = pos_delta ? static_cast<const int*>(pos_delta->data) : nullptr;
+  a.kv_s = kv_lens->strides[0];
+  a.new_s = new_lens->strides[0];
+  a.free_s = free_pages->strides[0];
+  a.delta_s = pos_delta ? pos_delta->strides[0] : 0;
+  a.bt = static_cast<int*>(block_table->data);
+  a.bt_sb = block_table->strides[0];
+  a.bt_sj = block_table->strides[1];
+  a.kv_out = static_cast<int*>(kv_lens_out->data);
+  a.used_out = static_cast<int*>(free_used_out->data);
+  a.indptr = static_cast<int*>(qo_indptr->data);
+  a.slots = static_cast<int64_t*>(slot_map->data);
+  a.pos = static_cast<int*>(positions->data);
+  a.kv_out_s = kv_lens_out->strides[0];
+  a.indptr_s = qo_indptr->strides[0];
+  a.slots_s = slot_map->strides[0];
+  a.pos_s = positions->strides[0];
+  a.B = (int)B;
+  a.rows = (int)rows;
+  a.n_free = (int)free_pages->shape[0];
+  a.num_pages = (int)num_pages;
+  a.page_size = (int)page_size;
+  while ((1 << a.log2_page) < page_size) ++a.log2_page;
+  a.max_pages = (int)max_pages;
+  a.err = w->err;
+  const hipError_t e = rl::launch_map(a, st);
+  if (e != hipSuccess) return hip_fail(e, "slot map kernel launch");
+  return RL_OK;
+}
+
+// ---------------------------------------------------------------- rotary rows
+// A tensor of head rows [rows, heads, 128] bf16, as the rotary kernels read or write it.
+int check_head_rows(const rl_tensor* t, const char* name, int64_t rows, int64_t heads, bool written) {
+  RL_TRY(check_view(t, name, 3));
+  RL_TRY(check_dtype(t, name, RL_BF16));
+  RL_TRY(check_rows128(t, name));
+  if (t->shape[0] != rows || t->shape[1] != heads)
+    return fail(RL_ERR_SHAPE, "%s must be [%lld, %lld, 128]", name, (long long)rows, (long long)heads);
+  if (written && ((rows > 1 && t->strides[0] < 128) || (heads > 1 && t->strides[1] < 128)))
+    return fail(RL_ERR_UNSUPPORTED, "%s: rows that are written must not overlap", name);
+  return check_data(t, name);
+}
+
+// Pages written at slots: as fill_paged, without a block table.
+int fill_slots(const rl_tensor* k, const rl_tensor* v, int kv_dtype, const rl_tensor* k_scale,
+               const rl_tensor* v_scale, int64_t Hkv, rl::RopeArgs* a) {
+  int one = 0;
+  rl_tensor bt{};                                   // (an empty table of no sequence)
+  bt.data = &one;
+  bt.dtype = RL_I32;
+  bt.ndim = 2;
+  bt.strides[0] = bt.strides[1] = 1;
+  rl::PagedKV kv{};
+  RL_TRY(fill_paged(k, v, &bt, 0, kv_dtype, k_scale, v_scale, &kv));
+  if (k->shape[2] != Hkv)
+    return fail(RL_ERR_SHAPE, "k_new has %lld KV heads, the pages %lld", (long long)Hkv, (long long)k->shape[2]);
+  a->k_pages = k->data;
+  a->v_pages = v->data;
+  a->kp_sp = kv.sp;
+  a->kp_ss = kv.ss;
+  a->kp_sh = kv.sh;
+  a->vp_sp = kv.v_sp;
+  a->vp_ss = kv.v_ss;
+  a->vp_sh = kv.v_sh;
+  a->k_scale = kv.k_scale;
+  a->v_scale = kv.v_scale;
+  a->ks_s = kv.ks_s;
+  a->vs_s = kv.vs_s;
+  a->num_pages = kv.num_pages;
+  a->page_size = kv.page_size;
+  a->log2_page = kv.log2_page;
+  return RL_OK;
+}
+
+int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const rl_tensor* positions,
+              const rl_tensor* inv_freq, const rl_tensor* axes, const rl_rope_opts* opts, const rl_tensor* slot_map,
+              rl_tensor* q_out, rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, bool append, int kv_dtype,
+              const rl_tensor* k_scale, const rl_tensor* v_scale, void* stream) {
+  rl::RopeArgs a{};
+  if (opts) {
+    for (int i = 0; i < 6; ++i)
+      if (opts->reserved[i] != 0) return fail(RL_ERR_INVALID_ARG, "opts.reserved[%d] must be zero", i);
+    if (opts->interleaved != 0 && opts->interleaved != 1)
+      return fail(RL_ERR_INVALID_ARG, "opts.interleaved must be 0 or 1");
+    if (opts->inverse != 0 && opts->inverse != 1) return fail(RL_ERR_INVALID_ARG, "opts.inverse must be 0 or 1");
+    if (opts->inverse && append) return fail(RL_ERR_INVALID_ARG, "opts.inverse is for rows that are not appended");
+    a.interleaved = opts->interleaved;
+    a.inverse = opts->inverse;
+  }
+  const char* k_name = append ? "k_new" : "k";
+  RL_TRY(check_view(q, "q", 3));
+  const int64_t rows = q->shape[0], Hq = q->shape[1];
+  RL_TRY(check_head_rows(q, "q", rows, Hq, false));
+  RL_TRY(check_head_rows(q_out, "q_out", rows, Hq, true));
+  int64_t Hkv = 0;
+  if (k || append) {
+    RL_TRY(check_view(k, k_name, 3));
+    Hkv = k->shape[1];
+    RL_TRY(check_head_rows(k, k_name, rows, Hkv, false));
+    if (append) RL_TRY(check_head_rows(v, "v_new", rows, Hkv, false));
+    if (k_out || !append) RL_TRY(check_head_rows(k_out, "k_out", rows, Hkv, true));
+  } else if (k_out) {
+    return fail(RL_ERR_INVALID_ARG, "k is NULL");
+  }
+  // (a launch has fewer than 2^32 threads, 64 for a row)
+  if (rows > (1 << 25) || Hq > 4096 || Hkv > 4096)
+    return fail(RL_ERR_UNSUPPORTED, "rows or head count too large");
+  RL_TRY(check_view(inv_freq, "inv_freq", 1));
+  const int64_t F = inv_freq->shape[0];
+  RL_TRY(check_vector(inv_freq, "inv_freq", RL_F32, F, false));
+  if (F < 8 || F > 64 || F % 8 != 0)
+    return fail(RL_ERR_UNSUPPORTED, "inv_freq must have a multiple of 8 entries, 8 to 64 (got %lld)", (long long)F);
+  RL_TRY(check_view(positions, "positions", 2));
+  RL_TRY(check_dtype(positions, "positions", RL_I32));
+  if (positions->shape[0] < 1 || positions->shape[0] > 64 || positions->shape[1] != rows)
+    return fail(RL_ERR_SHAPE, "positions must be [axes, rows] with 1 to 64 axes");
+  if (positions->strides[0] < 0 || positions->strides[1] < 0)
+    return fail(RL_ERR_UNSUPPORTED, "positions: strides must be non-negative");
+  RL_TRY(check_data(positions, "positions"));
+  if (axes) RL_TRY(check_vector(axes, "axes", RL_I32, F, false));
+  if (!axes && positions->shape[0] != 1)
+    return fail(RL_ERR_INVALID_ARG, "axes is NULL, but positions has %lld axes", (long long)positions->shape[0]);
+  if (append) {
+    RL_TRY(check_vector(slot_map, "slot_map", RL_I64, rows, false));
+    RL_TRY(fill_slots(k_pages, v_pages, kv_dtype, k_scale, v_scale, Hkv, &a));
+    a.slots = static_cast<const int64_t*>(slot_map->data);
+    a.slots_s = slot_map->strides[0];
+    a.v = v->data;
+    a.v_st = v->strides[0];
+    a.v_sh = v->strides[1];
+  }
+  if (rows == 0 || Hq + Hkv == 0) return RL_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
+  a.q = q->data;
+  a.q_st = q->strides[0];
+  a.q_sh = q->strides[1];
+  a.q_out = q_out->data;
+  a.qo_st = q_out->strides[0];
+  a.qo_sh = q_out->strides[1];
+  if (k) {
+    a.k = k->data;
+    a.k_st = k->strides[0];
+    a.k_sh = k->strides[1];
+  }
+  if (k_out) {
+    a.k_out = k_out->data;
+    a.ko_st = k_out->strides[0];
+    a.ko_sh = k_out->strides[1];
+  }
+  a.pos = static_cast<const int*>(positions->data);
+  a.pos_sa = positions->strides[0];
+  a.pos_st = positions->strides[1];
+  a.inv_freq = static_cast<const float*>(inv_freq->data);
+  a.freq_s = inv_freq->strides[0];
+  a.axes = axes ? static_cast<const int*>(axes->data) : nullptr;
+  a.axes_s = axes ? axes->strides[0] : 0;
+  a.rows = (int)rows;
+  a.Hq = (int)Hq;
+  a.Hkv = (int)Hkv;
+  a.freqs = (int)F;
+  a.n_axes = (int)positions->shape[0];
+  a.err = w->err;
+  rl::KernelTimer slot;
+  rl::KernelTimer* timer = prof_timer(&slot, st);
+  const hipError_t e = rl::launch_rope(a, st, timer);
+  prof_commit(4, timer);
+  if (e != hipSuccess) return hip_fail(e, "rotary kernel launch");
+  return RL_OK;
+}
+
+// -------------------------------------------------------------------- prefill
+int prefill_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const rl_tensor* seq_indptr, float scale,
+                 rl_tensor* out, rl_tensor* lse_out, void* stream) {
+  RL_TRY(check_scale(scale));
+  RL_TRY(check_view(q, "q", 3));
+  RL_TRY(check_dtype(q, "q", RL_BF16));
+  RL_TRY(check_rows128(q, "q"));
+  const int64_t rows = q->shape[0], Hq = q->shape[1];
+  RL_TRY(check_view(k, "k", 3));
+  const int64_t Hkv = k->shape[1];
+  if (Hkv < 1 || Hq < 1 || Hq % Hkv != 0)
+    return fail(RL_ERR_SHAPE, "query heads (%lld) must be a positive multiple of KV heads (%lld)", (long long)Hq,
+                (long long)Hkv);
+  RL_TRY(check_head_rows(k, "k", rows, Hkv, false));
+  RL_TRY(check_head_rows(v, "v", rows, Hkv, false));
+  RL_TRY(check_view(seq_indptr, "seq_indptr", 1));
+  const int64_t B = seq_indptr->shape[0] - 1;
+  if (B < 0) return fail(RL_ERR_SHAPE, "seq_indptr must have batch + 1 entries (got none)");
+  RL_TRY(check_vector(seq_indptr, "seq_indptr", RL_I32, B + 1, false));
+  int is_f32 = 0;
+  RL_TRY(check_out(out, q, "out", &is_f32));
+  RL_TRY(check_lse(lse_out, rows, Hq));
+  if (B > (1 << 22) || rows > INT32_MAX / 2 || Hq > 4096)
+    return fail(RL_ERR_UNSUPPORTED, "batch, rows or head count too large");
+  // in-prompt offsets are formed in 32 bits
+  const int64_t lim24 = (int64_t)1 << 24;
+  if (k->strides[0] >= lim24 || v->strides[0] >= lim24)
+    return fail(RL_ERR_UNSUPPORTED, "k/v: row strides must be < 2^24 elements");
+  RL_TRY(check_data(q, "q"));
+  if (B == 0 || rows == 0) return RL_OK;
+  rl::PrefillArgs a{};
+  const ExtendShape s = extend_shape(Hq / Hkv);
+  a.rows_head = s.rows_head;
+  a.tile_tokens = s.tile_tokens;
+  a.head_blocks = s.head_blocks;
+  // (a launch has fewer than 2^32 threads)
+  if ((rows / a.tile_tokens + B) * Hkv * a.head_blocks >= (1 << 23))
+    return fail(RL_ERR_UNSUPPORTED, "rows times heads too large");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
+  a.q = q->data;
+  a.q_st = q->strides[0];
+  a.q_sh = q->strides[1];
+  a.k = k->data;
+  a.k_st = k->strides[0];
+  a.k_sh = k->strides[1];
+  a.v = v->data;
+  a.v_st = v->strides[0];
+  a.v_sh = v->strides[1];
+  a.indptr = static_cast<const int*>(seq_indptr->data);
+  a.indptr_s = seq_indptr->strides[0];
+  a.B = (int)B;
+  a.rows = (int)rows;
+  a.Hq = (int)Hq;
+  a.Hkv = (int)Hkv;
+  a.R = (int)(Hq / Hkv);
+  a.scale = scale;
+  a.out = out->data;
+  a.out_f32 = is_f32;
+  a.out_st = out->strides[0];
+  a.out_sh = out->strides[1];
+  a.lse = lse_out ? static_cast<float*>(lse_out->data) : nullptr;
+  a.lse_st = lse_out ? lse_out->strides[0] : 0;
+  a.lse_sh = lse_out ? lse_out->strides[1] : 0;
+  a.err = w->err;
+  rl::KernelTimer slot;
+  rl::KernelTimer* timer = prof_timer(&slot, st);
+  const hipError_t e = rl::launch_prefill(a, st, timer);
+  prof_commit(3, timer);
+  if (e != hipSuccess) return hip_fail(e, "prefill kernel launch");
+  return RL_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1057,6 +1362,42 @@ int rl_attn_append_kv_fp8(const rl_tensor* k_new, const rl_tensor* v_new, const 
                           rl_tensor* v_pages, const rl_tensor* k_scale, const rl_tensor* v_scale, void* stream) {
   return append_impl(k_new, v_new, qo_indptr, block_table, kv_lens, k_pages, v_pages, RL_FP8_E4M3, k_scale, v_scale,
                      stream);
+}
+
+int rl_attn_map_slots(const rl_tensor* kv_lens, const rl_tensor* new_lens, const rl_tensor* free_pages,
+                      const rl_tensor* free_used, const rl_tensor* pos_delta, int64_t page_size, int64_t num_pages,
+                      rl_tensor* block_table, rl_tensor* kv_lens_out, rl_tensor* free_used_out, rl_tensor* qo_indptr,
+                      rl_tensor* slot_map, rl_tensor* positions, void* stream) {
+  return map_impl(kv_lens, new_lens, free_pages, free_used, pos_delta, page_size, num_pages, block_table, kv_lens_out,
+                  free_used_out, qo_indptr, slot_map, positions, stream);
+}
+
+int rl_attn_rope(const rl_tensor* q, const rl_tensor* k, const rl_tensor* positions, const rl_tensor* inv_freq,
+                 const rl_tensor* axes, const rl_rope_opts* opts, rl_tensor* q_out, rl_tensor* k_out, void* stream) {
+  return rope_impl(q, k, nullptr, positions, inv_freq, axes, opts, nullptr, q_out, k_out, nullptr, nullptr, false,
+                   RL_BF16, nullptr, nullptr, stream);
+}
+
+int rl_attn_rope_append_kv(const rl_tensor* q, const rl_tensor* k_new, const rl_tensor* v_new,
+                           const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                           const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out, rl_tensor* k_out,
+                           rl_tensor* k_pages, rl_tensor* v_pages, void* stream) {
+  return rope_impl(q, k_new, v_new, positions, inv_freq, axes, opts, slot_map, q_out, k_out, k_pages, v_pages, true,
+                   RL_BF16, nullptr, nullptr, stream);
+}
+
+int rl_attn_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const rl_tensor* v_new,
+                               const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                               const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out,
+                               rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, const rl_tensor* k_scale,
+                               const rl_tensor* v_scale, void* stream) {
+  return rope_impl(q, k_new, v_new, positions, inv_freq, axes, opts, slot_map, q_out, k_out, k_pages, v_pages, true,
+                   RL_FP8_E4M3, k_scale, v_scale, stream);
+}
+
+int rl_attn_prefill(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const rl_tensor* seq_indptr,
+                    float scale, rl_tensor* out, rl_tensor* lse_out, void* stream) {
+  return prefill_impl(q, k, v, seq_indptr, scale, out, lse_out, stream);
 }
 
 int rl_attn_merge(const rl_tensor* o_parts, const rl_tensor* lse_parts, const rl_tensor* num_parts, rl_tensor* out,
@@ -1151,6 +1492,10 @@ int rl_attn_check_device_errors(void* stream) {
     if (word & rl::kErrKvShort) what += " kv_lens-shorter-than-chunk";
     if (word & rl::kErrScale) what += " dequant-scale-invalid";
     if (word & rl::kErrCapacity) what += " workspace-capacity-exceeded";
+    if (word & rl::kErrRows) what += " rows-past-slot-map";
+    if (word & rl::kErrPool) what += " free-pages-exhausted";
+    if (word & rl::kErrSlot) what += " slot-out-of-range";
+    if (word & rl::kErrAxis) what += " position-axis-out-of-range";
     return fail(RL_ERR_DEVICE, "device-side input errors (values were clamped):%s", what.c_str());
   }
   return RL_OK;
@@ -1393,7 +1738,8 @@ int rl_attn_profile_enable(int on) {
 }
 
 int rl_attn_profile_read(int kind, int* launches, double* mean_ms) {
-  if (kind < 0 || kind > 2) return fail(RL_ERR_INVALID_ARG, "kind must be 0 (decode), 1 (extend) or 2 (append)");
+  if (kind < 0 || kind > 4)
+    return fail(RL_ERR_INVALID_ARG, "kind must be 0 (decode), 1 (extend), 2 (append), 3 (prefill) or 4 (rotary rows)");
   if (!launches || !mean_ms) return fail(RL_ERR_INVALID_ARG, "launches and mean_ms must not be NULL");
   std::vector<rl::KernelTimer> ts;
   {

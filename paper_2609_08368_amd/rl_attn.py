@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -21,7 +21,7 @@ LIB_PATH = os.environ.get("RL_ATTN_LIB", os.path.join(_PKG, "librlattn.so"))
 INCLUDE = os.path.join(os.path.dirname(_PKG), "include")
 HEADER = os.path.join(INCLUDE, "rl_attn.h")
 
-RL_BF16, RL_F32, RL_I32, RL_FP8_E4M3 = 1, 2, 3, 4
+RL_BF16, RL_F32, RL_I32, RL_FP8_E4M3, RL_I64 = 1, 2, 3, 4, 5
 RL_PREFIX_AUTO, RL_PREFIX_OFF = 0, 1
 STATUS = {
     0: "RL_OK", -1: "RL_ERR_INVALID_ARG", -2: "RL_ERR_SHAPE", -3: "RL_ERR_DTYPE", -4: "RL_ERR_UNSUPPORTED",
@@ -38,6 +38,10 @@ class RlTensor(ctypes.Structure):
 class RlOpts(ctypes.Structure):
     _fields_ = [("split_tokens", ctypes.c_int32), ("prefix_share", ctypes.c_int32),
                 ("validate", ctypes.c_int32), ("deterministic", ctypes.c_int32), ("reserved", ctypes.c_int32 * 4)]
+
+
+class RlRopeOpts(ctypes.Structure):
+    _fields_ = [("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32), ("reserved", ctypes.c_int32 * 6)]
 
 
 class RlAttnError(RuntimeError):
@@ -68,6 +72,12 @@ def lib() -> ctypes.CDLL:
         L.rl_attn_extend_fp8.argtypes = [P, P, P, P, P, P, P, P, ctypes.c_float, P, P, ctypes.POINTER(RlOpts), vp]
         L.rl_attn_append_kv.argtypes = [P, P, P, P, P, P, P, vp]
         L.rl_attn_append_kv_fp8.argtypes = [P, P, P, P, P, P, P, P, P, vp]
+        L.rl_attn_map_slots.argtypes = [P, P, P, P, P, ctypes.c_int64, ctypes.c_int64, P, P, P, P, P, P, vp]
+        R = ctypes.POINTER(RlRopeOpts)
+        L.rl_attn_rope.argtypes = [P, P, P, P, P, R, P, P, vp]
+        L.rl_attn_rope_append_kv.argtypes = [P, P, P, P, P, P, R, P, P, P, P, P, vp]
+        L.rl_attn_rope_append_kv_fp8.argtypes = [P, P, P, P, P, P, R, P, P, P, P, P, P, P, vp]
+        L.rl_attn_prefill.argtypes = [P, P, P, P, ctypes.c_float, P, P, vp]
         L.rl_attn_merge.argtypes = [P, P, P, P, P, vp]
         L.rl_attn_last_error.restype = ctypes.c_char_p
         L.rl_attn_check_device_errors.argtypes = [vp]
@@ -89,7 +99,8 @@ def lib() -> ctypes.CDLL:
         for name in ("rl_attn_decode", "rl_attn_extend", "rl_attn_decode_ex", "rl_attn_extend_ex",
                      "rl_attn_decode_noalloc",
                      "rl_attn_decode_fp8", "rl_attn_extend_fp8", "rl_attn_append_kv", "rl_attn_append_kv_fp8",
-                     "rl_attn_merge", "rl_attn_check_device_errors", "rl_attn_reserve_workspace",
+                     "rl_attn_map_slots", "rl_attn_rope", "rl_attn_rope_append_kv", "rl_attn_rope_append_kv_fp8",
+                     "rl_attn_prefill", "rl_attn_merge", "rl_attn_check_device_errors", "rl_attn_reserve_workspace",
                      "rl_attn_profile_enable", "rl_attn_profile_read", "rl_attn_diag_read_bandwidth",
                      "rl_attn_diag_mfma_bf16", "rl_attn_diag_decode_capacity", "rl_attn_diag_extend_capacity",
                      "rl_attn_diag_extend_plan"):
@@ -119,7 +130,7 @@ def _check(rc: int):
 
 
 _DTYPES = {torch.bfloat16: RL_BF16, torch.float32: RL_F32, torch.int32: RL_I32,
-           torch.float8_e4m3fn: RL_FP8_E4M3}
+           torch.float8_e4m3fn: RL_FP8_E4M3, torch.int64: RL_I64}
 
 
 def view(t: Optional[torch.Tensor]):
@@ -262,6 +273,97 @@ def append_kv_fp8(k_new, v_new, qo_indptr, block_table, kv_lens, k_pages, v_page
                                        _stream(stream)))
 
 
+class SlotMap(NamedTuple):
+    """What ``map_slots`` gives for a step (the block table is written in place)."""
+
+    qo_indptr: torch.Tensor
+    slot_map: torch.Tensor
+    positions: torch.Tensor
+    kv_lens: torch.Tensor
+    free_used: torch.Tensor
+
+
+def map_slots(kv_lens, new_lens, free_pages, free_used, block_table, page_size, num_pages, rows=None, *,
+              pos_delta=None, kv_lens_out=None, free_used_out=None, qo_indptr=None, slot_map=None, positions=None,
+              stream=None) -> SlotMap:
+    """``rl_attn_map_slots``: ``rows`` is the length of a ``slot_map`` and ``positions`` that are not given.
+
+    ``kv_lens_out=kv_lens, free_used_out=free_used`` advances a step in place."""
+    dev = kv_lens.device
+    if slot_map is None:
+        if rows is None:
+            raise ValueError("rows is needed where slot_map is not given")
+        slot_map = torch.empty(rows, dtype=torch.int64, device=dev)
+    if positions is None:
+        positions = torch.empty(slot_map.shape[0], dtype=torch.int32, device=dev)
+    if qo_indptr is None:
+        qo_indptr = torch.empty(kv_lens.shape[0] + 1, dtype=torch.int32, device=dev)
+    if kv_lens_out is None:
+        kv_lens_out = torch.empty_like(kv_lens)
+    if free_used_out is None:
+        free_used_out = torch.empty_like(free_used)
+    _check(lib().rl_attn_map_slots(_ref(view(kv_lens)), _ref(view(new_lens)), _ref(view(free_pages)),
+                                   _ref(view(free_used)), _ref(view(pos_delta)), page_size, num_pages,
+                                   _ref(view(block_table)), _ref(view(kv_lens_out)), _ref(view(free_used_out)),
+                                   _ref(view(qo_indptr)), _ref(view(slot_map)), _ref(view(positions)),
+                                   _stream(stream)))
+    return SlotMap(qo_indptr, slot_map, positions, kv_lens_out, free_used_out)
+
+
+def _rope_opts(interleaved, inverse=False):
+    o = RlRopeOpts()
+    o.interleaved = int(bool(interleaved))
+    o.inverse = int(bool(inverse))
+    return ctypes.byref(o)
+
+
+def rope(q, k, positions, inv_freq, axes=None, *, interleaved=False, inverse=False, q_out=None, k_out=None,
+         stream=None):
+    """``rl_attn_rope``: returns ``(q_out, k_out)`` (``k`` may be None). ``q_out=q, k_out=k`` rotates in place."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None and k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    _check(lib().rl_attn_rope(_ref(view(q)), _ref(view(k)), _ref(view(positions)), _ref(view(inv_freq)),
+                              _ref(view(axes)), _rope_opts(interleaved, inverse), _ref(view(q_out)),
+                              _ref(view(k_out)), _stream(stream)))
+    return q_out, k_out
+
+
+def rope_append_kv(q, k_new, v_new, positions, inv_freq, slot_map, k_pages, v_pages, axes=None, *, interleaved=False,
+                   q_out=None, k_out=None, stream=None):
+    """``rl_attn_rope_append_kv``: returns ``q_out``; ``k_out`` (rows of rotated keys) is written only if given."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(lib().rl_attn_rope_append_kv(_ref(view(q)), _ref(view(k_new)), _ref(view(v_new)), _ref(view(positions)),
+                                        _ref(view(inv_freq)), _ref(view(axes)), _rope_opts(interleaved),
+                                        _ref(view(slot_map)), _ref(view(q_out)), _ref(view(k_out)),
+                                        _ref(view(k_pages)), _ref(view(v_pages)), _stream(stream)))
+    return q_out
+
+
+def rope_append_kv_fp8(q, k_new, v_new, positions, inv_freq, slot_map, k_pages, v_pages, k_scale, v_scale, axes=None,
+                       *, interleaved=False, q_out=None, k_out=None, stream=None):
+    """``rl_attn_rope_append_kv_fp8``: as ``rope_append_kv`` into ``torch.float8_e4m3fn`` pages."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(lib().rl_attn_rope_append_kv_fp8(_ref(view(q)), _ref(view(k_new)), _ref(view(v_new)),
+                                            _ref(view(positions)), _ref(view(inv_freq)), _ref(view(axes)),
+                                            _rope_opts(interleaved), _ref(view(slot_map)), _ref(view(q_out)),
+                                            _ref(view(k_out)), _ref(view(k_pages)), _ref(view(v_pages)),
+                                            _ref(view(k_scale)), _ref(view(v_scale)), _stream(stream)))
+    return q_out
+
+
+def prefill(q, k, v, seq_indptr, scale, out=None, lse=None, *, stream=None):
+    """``rl_attn_prefill``: causal attention over packed prompts; returns ``out`` (and fills ``lse`` if given)."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(lib().rl_attn_prefill(_ref(view(q)), _ref(view(k)), _ref(view(v)), _ref(view(seq_indptr)),
+                                 ctypes.c_float(scale), _ref(view(out)), _ref(view(lse)), _stream(stream)))
+    return out
+
+
 def merge(o_parts, lse_parts, num_parts, out=None, lse=None, stream=None):
     """``rl_attn_merge``: log-sum-exp merge of partial results."""
     n, _, h, d = o_parts.shape
@@ -297,10 +399,11 @@ def profile_enable(on: bool = True):
 
 
 def profile_read(kind: str):
-    """(launches, mean ms) of the main kernel timed since the last read; kind 'decode', 'extend' or 'append'."""
+    """(launches, mean ms) of the main kernel timed since the last read; kind 'decode', 'extend', 'append',
+    'prefill' or 'rope'."""
     n = ctypes.c_int()
     ms = ctypes.c_double()
-    _check(lib().rl_attn_profile_read({"decode": 0, "extend": 1, "append": 2}[kind], ctypes.byref(n),
+    _check(lib().rl_attn_profile_read({"decode": 0, "extend": 1, "append": 2, "prefill": 3, "rope": 4}[kind], ctypes.byref(n),
                                       ctypes.byref(ms)))
     return n.value, ms.value
 
