@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -61,8 +62,8 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is not built; run __graft_entry__.build() first")
         L = ctypes.CDLL(LIB_PATH)
-        P = ctypes.POINTER(RlTensor)
         vp = ctypes.c_void_p
+        P = vp                                  # rl_tensor: the bytes of one (_arg), or a reference to one
         L.rl_attn_decode.argtypes = [P, P, P, P, P, ctypes.c_float, P, vp]
         L.rl_attn_extend.argtypes = [P, P, P, P, P, P, ctypes.c_float, P, vp]
         L.rl_attn_decode_ex.argtypes = [P, P, P, P, P, ctypes.c_float, P, P, ctypes.POINTER(RlOpts), vp]
@@ -133,35 +134,42 @@ _DTYPES = {torch.bfloat16: RL_BF16, torch.float32: RL_F32, torch.int32: RL_I32,
            torch.float8_e4m3fn: RL_FP8_E4M3, torch.int64: RL_I64}
 
 
-def view(t: Optional[torch.Tensor]):
-    """An ``rl_tensor`` describing ``t`` (no copy); None -> NULL.
+# rl_tensor of 1 to 4 dimensions, the unused shape and stride entries zero
+_LAYOUT = {n: struct.Struct(f"=Qii{n}q{32 - 8 * n}x{n}q{32 - 8 * n}x") for n in range(5)}
+# (the functions behind torch.cuda.current_device() and current_stream(), without what those do besides: 0.1 us
+# instead of 0.2 us for each tensor and 3 us for the stream, of calls whose kernels take 5 us)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                          lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _arg(t: Optional[torch.Tensor]) -> Optional[bytes]:
+    """The bytes of an ``rl_tensor`` describing ``t`` (no copy of its data); None -> NULL.
 
     The library dereferences the pointers on the current HIP device, so every
     tensor must live there (a host pointer would reach a kernel)."""
     if t is None:
         return None
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    device = t.get_device()
+    if device < 0 or device != _current_device():
         raise ValueError(f"tensor on {t.device}: the library reads and writes tensors on the current device "
                          f"(cuda:{torch.cuda.current_device() if torch.cuda.is_available() else '?'})")
-    if t.dim() > 4:
+    n = t.dim()
+    if n > 4:
         raise ValueError("rl_tensor holds at most 4 dimensions")
-    v = RlTensor()
-    v.data = t.data_ptr() if t.numel() else (t.data_ptr() or None)
-    v.dtype = _DTYPES.get(t.dtype, 0)
-    v.ndim = t.dim()
-    for i in range(t.dim()):
-        v.shape[i] = t.shape[i]
-        v.strides[i] = t.stride(i)
-    return v
+    return _LAYOUT[n].pack(t.data_ptr(), _DTYPES.get(t.dtype, 0), n, *t.shape, *t.stride())
 
 
-def _ref(v):
-    return ctypes.byref(v) if v is not None else None
+def view(t: Optional[torch.Tensor]):
+    """An ``rl_tensor`` describing ``t`` (no copy); None -> NULL."""
+    return None if t is None else RlTensor.from_buffer_copy(_arg(t))
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        if not torch.cuda.is_initialized():
+            torch.cuda.init()
+        return _current_stream(_current_device())
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -180,9 +188,9 @@ def decode(q, k_pages, v_pages, block_table, seq_lens, scale, out=None, lse=None
     if out is None:
         out = torch.empty_like(q)
     o = _opts(split_tokens, prefix_share, validate, deterministic)
-    _check(lib().rl_attn_decode_ex(_ref(view(q)), _ref(view(k_pages)), _ref(view(v_pages)),
-                                   _ref(view(block_table)), _ref(view(seq_lens)), ctypes.c_float(scale),
-                                   _ref(view(out)), _ref(view(lse)), ctypes.byref(o), _stream(stream)))
+    _check(lib().rl_attn_decode_ex(_arg(q), _arg(k_pages), _arg(v_pages), _arg(block_table), _arg(seq_lens),
+                                   ctypes.c_float(scale), _arg(out), _arg(lse), ctypes.byref(o),
+                                   _stream(stream)))
     return out
 
 
@@ -193,9 +201,9 @@ def decode_noalloc(q, k_pages, v_pages, block_table, seq_lens, scale, out=None, 
     if out is None:
         out = torch.empty_like(q)
     o = _opts(split_tokens, prefix_share, False, deterministic)
-    _check(lib().rl_attn_decode_noalloc(_ref(view(q)), _ref(view(k_pages)), _ref(view(v_pages)),
-                                        _ref(view(block_table)), _ref(view(seq_lens)), ctypes.c_float(scale),
-                                        _ref(view(out)), _ref(view(lse)), ctypes.byref(o), _stream(stream)))
+    _check(lib().rl_attn_decode_noalloc(_arg(q), _arg(k_pages), _arg(v_pages), _arg(block_table),
+                                        _arg(seq_lens), ctypes.c_float(scale), _arg(out), _arg(lse),
+                                        ctypes.byref(o), _stream(stream)))
     return out
 
 
@@ -203,9 +211,8 @@ def decode_plain(q, k_pages, v_pages, block_table, seq_lens, scale, out=None, st
     """``rl_attn_decode`` (the fixed signature, no options)."""
     if out is None:
         out = torch.empty_like(q)
-    _check(lib().rl_attn_decode(_ref(view(q)), _ref(view(k_pages)), _ref(view(v_pages)),
-                                _ref(view(block_table)), _ref(view(seq_lens)), ctypes.c_float(scale),
-                                _ref(view(out)), _stream(stream)))
+    _check(lib().rl_attn_decode(_arg(q), _arg(k_pages), _arg(v_pages), _arg(block_table), _arg(seq_lens),
+                                ctypes.c_float(scale), _arg(out), _stream(stream)))
     return out
 
 
@@ -215,9 +222,8 @@ def extend(q, qo_indptr, k_pages, v_pages, block_table, kv_lens, scale, out=None
     if out is None:
         out = torch.empty_like(q)
     o = _opts(0, True, validate)
-    _check(lib().rl_attn_extend_ex(_ref(view(q)), _ref(view(qo_indptr)), _ref(view(k_pages)),
-                                   _ref(view(v_pages)), _ref(view(block_table)), _ref(view(kv_lens)),
-                                   ctypes.c_float(scale), _ref(view(out)), _ref(view(lse)), ctypes.byref(o),
+    _check(lib().rl_attn_extend_ex(_arg(q), _arg(qo_indptr), _arg(k_pages), _arg(v_pages), _arg(block_table),
+                                   _arg(kv_lens), ctypes.c_float(scale), _arg(out), _arg(lse), ctypes.byref(o),
                                    _stream(stream)))
     return out
 
@@ -226,9 +232,8 @@ def extend_plain(q, qo_indptr, k_pages, v_pages, block_table, kv_lens, scale, ou
     """``rl_attn_extend`` (the fixed signature)."""
     if out is None:
         out = torch.empty_like(q)
-    _check(lib().rl_attn_extend(_ref(view(q)), _ref(view(qo_indptr)), _ref(view(k_pages)), _ref(view(v_pages)),
-                                _ref(view(block_table)), _ref(view(kv_lens)), ctypes.c_float(scale),
-                                _ref(view(out)), _stream(stream)))
+    _check(lib().rl_attn_extend(_arg(q), _arg(qo_indptr), _arg(k_pages), _arg(v_pages), _arg(block_table),
+                                _arg(kv_lens), ctypes.c_float(scale), _arg(out), _stream(stream)))
     return out
 
 
@@ -238,10 +243,9 @@ def decode_fp8(q, k_pages, v_pages, k_scale, v_scale, block_table, seq_lens, sca
     if out is None:
         out = torch.empty_like(q)
     o = _opts(split_tokens, prefix_share, validate, deterministic)
-    _check(lib().rl_attn_decode_fp8(_ref(view(q)), _ref(view(k_pages)), _ref(view(v_pages)), _ref(view(k_scale)),
-                                    _ref(view(v_scale)), _ref(view(block_table)), _ref(view(seq_lens)),
-                                    ctypes.c_float(scale), _ref(view(out)), _ref(view(lse)), ctypes.byref(o),
-                                    _stream(stream)))
+    _check(lib().rl_attn_decode_fp8(_arg(q), _arg(k_pages), _arg(v_pages), _arg(k_scale), _arg(v_scale),
+                                    _arg(block_table), _arg(seq_lens), ctypes.c_float(scale), _arg(out),
+                                    _arg(lse), ctypes.byref(o), _stream(stream)))
     return out
 
 
@@ -251,26 +255,23 @@ def extend_fp8(q, qo_indptr, k_pages, v_pages, k_scale, v_scale, block_table, kv
     if out is None:
         out = torch.empty_like(q)
     o = _opts(0, True, validate)
-    _check(lib().rl_attn_extend_fp8(_ref(view(q)), _ref(view(qo_indptr)), _ref(view(k_pages)), _ref(view(v_pages)),
-                                    _ref(view(k_scale)), _ref(view(v_scale)), _ref(view(block_table)),
-                                    _ref(view(kv_lens)), ctypes.c_float(scale), _ref(view(out)), _ref(view(lse)),
-                                    ctypes.byref(o), _stream(stream)))
+    _check(lib().rl_attn_extend_fp8(_arg(q), _arg(qo_indptr), _arg(k_pages), _arg(v_pages), _arg(k_scale),
+                                    _arg(v_scale), _arg(block_table), _arg(kv_lens), ctypes.c_float(scale),
+                                    _arg(out), _arg(lse), ctypes.byref(o), _stream(stream)))
     return out
 
 
 def append_kv(k_new, v_new, qo_indptr, block_table, kv_lens, k_pages, v_pages, stream=None):
     """``rl_attn_append_kv``: writes the new rows into ``k_pages``/``v_pages`` (in place)."""
-    _check(lib().rl_attn_append_kv(_ref(view(k_new)), _ref(view(v_new)), _ref(view(qo_indptr)),
-                                   _ref(view(block_table)), _ref(view(kv_lens)), _ref(view(k_pages)),
-                                   _ref(view(v_pages)), _stream(stream)))
+    _check(lib().rl_attn_append_kv(_arg(k_new), _arg(v_new), _arg(qo_indptr), _arg(block_table), _arg(kv_lens),
+                                   _arg(k_pages), _arg(v_pages), _stream(stream)))
 
 
 def append_kv_fp8(k_new, v_new, qo_indptr, block_table, kv_lens, k_pages, v_pages, k_scale, v_scale, stream=None):
     """``rl_attn_append_kv_fp8``: bf16 rows quantised into ``torch.float8_e4m3fn`` pages (in place)."""
-    _check(lib().rl_attn_append_kv_fp8(_ref(view(k_new)), _ref(view(v_new)), _ref(view(qo_indptr)),
-                                       _ref(view(block_table)), _ref(view(kv_lens)), _ref(view(k_pages)),
-                                       _ref(view(v_pages)), _ref(view(k_scale)), _ref(view(v_scale)),
-                                       _stream(stream)))
+    _check(lib().rl_attn_append_kv_fp8(_arg(k_new), _arg(v_new), _arg(qo_indptr), _arg(block_table),
+                                       _arg(kv_lens), _arg(k_pages), _arg(v_pages), _arg(k_scale),
+                                       _arg(v_scale), _stream(stream)))
 
 
 class SlotMap(NamedTuple):
@@ -302,19 +303,18 @@ def map_slots(kv_lens, new_lens, free_pages, free_used, block_table, page_size, 
         kv_lens_out = torch.empty_like(kv_lens)
     if free_used_out is None:
         free_used_out = torch.empty_like(free_used)
-    _check(lib().rl_attn_map_slots(_ref(view(kv_lens)), _ref(view(new_lens)), _ref(view(free_pages)),
-                                   _ref(view(free_used)), _ref(view(pos_delta)), page_size, num_pages,
-                                   _ref(view(block_table)), _ref(view(kv_lens_out)), _ref(view(free_used_out)),
-                                   _ref(view(qo_indptr)), _ref(view(slot_map)), _ref(view(positions)),
+    _check(lib().rl_attn_map_slots(_arg(kv_lens), _arg(new_lens), _arg(free_pages), _arg(free_used),
+                                   _arg(pos_delta), page_size, num_pages, _arg(block_table), _arg(kv_lens_out),
+                                   _arg(free_used_out), _arg(qo_indptr), _arg(slot_map), _arg(positions),
                                    _stream(stream)))
     return SlotMap(qo_indptr, slot_map, positions, kv_lens_out, free_used_out)
 
 
+_ROPE_OPTS = {(i, b): RlRopeOpts(interleaved=i, inverse=b) for i in (0, 1) for b in (0, 1)}
+
+
 def _rope_opts(interleaved, inverse=False):
-    o = RlRopeOpts()
-    o.interleaved = int(bool(interleaved))
-    o.inverse = int(bool(inverse))
-    return ctypes.byref(o)
+    return ctypes.byref(_ROPE_OPTS[bool(interleaved), bool(inverse)])
 
 
 def rope(q, k, positions, inv_freq, axes=None, *, interleaved=False, inverse=False, q_out=None, k_out=None,
@@ -324,9 +324,8 @@ def rope(q, k, positions, inv_freq, axes=None, *, interleaved=False, inverse=Fal
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if k_out is None and k is not None:
         k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    _check(lib().rl_attn_rope(_ref(view(q)), _ref(view(k)), _ref(view(positions)), _ref(view(inv_freq)),
-                              _ref(view(axes)), _rope_opts(interleaved, inverse), _ref(view(q_out)),
-                              _ref(view(k_out)), _stream(stream)))
+    _check(lib().rl_attn_rope(_arg(q), _arg(k), _arg(positions), _arg(inv_freq), _arg(axes),
+                              _rope_opts(interleaved, inverse), _arg(q_out), _arg(k_out), _stream(stream)))
     return q_out, k_out
 
 
@@ -335,10 +334,9 @@ def rope_append_kv(q, k_new, v_new, positions, inv_freq, slot_map, k_pages, v_pa
     """``rl_attn_rope_append_kv``: returns ``q_out``; ``k_out`` (rows of rotated keys) is written only if given."""
     if q_out is None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _check(lib().rl_attn_rope_append_kv(_ref(view(q)), _ref(view(k_new)), _ref(view(v_new)), _ref(view(positions)),
-                                        _ref(view(inv_freq)), _ref(view(axes)), _rope_opts(interleaved),
-                                        _ref(view(slot_map)), _ref(view(q_out)), _ref(view(k_out)),
-                                        _ref(view(k_pages)), _ref(view(v_pages)), _stream(stream)))
+    _check(lib().rl_attn_rope_append_kv(_arg(q), _arg(k_new), _arg(v_new), _arg(positions), _arg(inv_freq),
+                                        _arg(axes), _rope_opts(interleaved), _arg(slot_map), _arg(q_out),
+                                        _arg(k_out), _arg(k_pages), _arg(v_pages), _stream(stream)))
     return q_out
 
 
@@ -347,11 +345,10 @@ def rope_append_kv_fp8(q, k_new, v_new, positions, inv_freq, slot_map, k_pages, 
     """``rl_attn_rope_append_kv_fp8``: as ``rope_append_kv`` into ``torch.float8_e4m3fn`` pages."""
     if q_out is None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _check(lib().rl_attn_rope_append_kv_fp8(_ref(view(q)), _ref(view(k_new)), _ref(view(v_new)),
-                                            _ref(view(positions)), _ref(view(inv_freq)), _ref(view(axes)),
-                                            _rope_opts(interleaved), _ref(view(slot_map)), _ref(view(q_out)),
-                                            _ref(view(k_out)), _ref(view(k_pages)), _ref(view(v_pages)),
-                                            _ref(view(k_scale)), _ref(view(v_scale)), _stream(stream)))
+    _check(lib().rl_attn_rope_append_kv_fp8(_arg(q), _arg(k_new), _arg(v_new), _arg(positions), _arg(inv_freq),
+                                            _arg(axes), _rope_opts(interleaved), _arg(slot_map), _arg(q_out),
+                                            _arg(k_out), _arg(k_pages), _arg(v_pages), _arg(k_scale),
+                                            _arg(v_scale), _stream(stream)))
     return q_out
 
 
@@ -359,8 +356,8 @@ def prefill(q, k, v, seq_indptr, scale, out=None, lse=None, *, stream=None):
     """``rl_attn_prefill``: causal attention over packed prompts; returns ``out`` (and fills ``lse`` if given)."""
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _check(lib().rl_attn_prefill(_ref(view(q)), _ref(view(k)), _ref(view(v)), _ref(view(seq_indptr)),
-                                 ctypes.c_float(scale), _ref(view(out)), _ref(view(lse)), _stream(stream)))
+    _check(lib().rl_attn_prefill(_arg(q), _arg(k), _arg(v), _arg(seq_indptr), ctypes.c_float(scale), _arg(out),
+                                 _arg(lse), _stream(stream)))
     return out
 
 
@@ -369,8 +366,8 @@ def merge(o_parts, lse_parts, num_parts, out=None, lse=None, stream=None):
     n, _, h, d = o_parts.shape
     if out is None:
         out = torch.empty((n, h, d), dtype=torch.float32, device=o_parts.device)
-    _check(lib().rl_attn_merge(_ref(view(o_parts)), _ref(view(lse_parts)), _ref(view(num_parts)),
-                               _ref(view(out)), _ref(view(lse)), _stream(stream)))
+    _check(lib().rl_attn_merge(_arg(o_parts), _arg(lse_parts), _arg(num_parts), _arg(out), _arg(lse),
+                               _stream(stream)))
     return out
 
 
@@ -403,8 +400,8 @@ def profile_read(kind: str):
     'prefill' or 'rope'."""
     n = ctypes.c_int()
     ms = ctypes.c_double()
-    _check(lib().rl_attn_profile_read({"decode": 0, "extend": 1, "append": 2, "prefill": 3, "rope": 4}[kind], ctypes.byref(n),
-                                      ctypes.byref(ms)))
+    _check(lib().rl_attn_profile_read({"decode": 0, "extend": 1, "append": 2, "prefill": 3, "rope": 4}[kind],
+                                      ctypes.byref(n), ctypes.byref(ms)))
     return n.value, ms.value
 
 
@@ -416,7 +413,7 @@ def diag_read_bandwidth(buf: torch.Tensor, reps: int = 10, stream=None) -> float
     """HBM read rate (GB/s) of streaming ``buf`` (a device tensor) ``reps`` times."""
     r = ctypes.c_double(0.0)
     _check(lib().rl_attn_diag_read_bandwidth(ctypes.c_void_p(buf.data_ptr()), buf.numel() * buf.element_size(),
-                                            reps, ctypes.byref(r), _stream(stream)))
+                                             reps, ctypes.byref(r), _stream(stream)))
     return r.value
 
 
@@ -431,8 +428,9 @@ def diag_decode_capacity(batch, num_q_heads, num_kv_heads, max_pages, page_size,
                          prefix_share=True, cus=256, workers_per_cu=1) -> dict:
     """Workspace capacities a decode call would be given (host arithmetic only)."""
     out = (ctypes.c_int64 * 7)()
-    _check(lib().rl_attn_diag_decode_capacity(batch, num_q_heads, num_kv_heads, max_pages, page_size, query_tokens,
-                                              split_tokens, int(bool(prefix_share)), cus, workers_per_cu, out))
+    _check(lib().rl_attn_diag_decode_capacity(batch, num_q_heads, num_kv_heads, max_pages, page_size,
+                                              query_tokens, split_tokens, int(bool(prefix_share)), cus,
+                                              workers_per_cu, out))
     keys = ("max_items", "max_slots", "max_workers", "group_cap", "target_items", "prefix_grid", "bytes")
     return dict(zip(keys, (int(x) for x in out)))
 
@@ -454,7 +452,7 @@ def diag_extend_plan(kv_lens, num_q_heads, num_kv_heads, max_tokens, qo_indptr=N
     if total_q is None:
         total_q = b * query_tokens if qo_indptr is None else int(qo_indptr[-1])
     out = (ctypes.c_int64 * 8)()
-    _check(lib().rl_attn_diag_extend_plan(ind, lens, b, total_q, query_tokens, num_q_heads, num_kv_heads, max_tokens,
-                                          cus, out))
+    _check(lib().rl_attn_diag_extend_plan(ind, lens, b, total_q, query_tokens, num_q_heads, num_kv_heads,
+                                          max_tokens, cus, out))
     keys = ("items", "parts", "split_seqs", "split_units", "broken_units", "errors", "max_units", "mode")
     return dict(zip(keys, (int(x) for x in out)))
