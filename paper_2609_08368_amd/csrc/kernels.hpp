@@ -298,9 +298,11 @@ struct PrefillArgs {
   const int* indptr;      // [B + 1]
   int64_t indptr_s;
   int B, rows, Hq, Hkv, R;
+  int tile_rows;          // query rows per tile: 128 or 256
   int rows_head;          // query heads per tile
   int tile_tokens;        // prompt tokens per tile
   int head_blocks;        // ceil(R / rows_head)
+  int chunk_log;          // log2 of the tiles that are neighbours in the order of the units
   float scale;
   void* out;
   int out_f32;
@@ -345,6 +347,6 @@ hipError_t launch_merge(const MergeArgs& a, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream, KernelTimer* timer);
 hipError_t launch_map(const MapArgs& a, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream, KernelTimer* timer);
-hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream, KernelTimer* timer);
+hipError_t launch_prefill(const PrefillArgs& a, int cus, hipStream_t stream, KernelTimer* timer);
 
 }  // namespace rl

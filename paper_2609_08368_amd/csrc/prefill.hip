@@ -3,8 +3,9 @@
 //
 // A unit of work is (prompt b, KV head g, block of query heads, run of tokens):
 // up to 256 query rows, token-major (row r -> token r / RB, head r % RB), which
-// all read the same keys; one workgroup computes it.
+// all read the same keys.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.hpp"
 #include "tile_attn.hpp"
@@ -13,7 +14,39 @@ namespace rl {
 
 namespace {
 
-constexpr int kPreWaves = 8;
+constexpr int kPreThreads = 256;       // four waves, one a SIMD
+constexpr int kStep = 64;              // keys of a step
+constexpr int kAhead = 4, kRing = 8;   // LDS operands read ahead of their MFMAs, and their registers
+constexpr int kKPitch = 1024 + 16;     // LDS blocks of four 256-byte rows
+constexpr int kVPitch = 1024 + 64;
+constexpr int kKSize = 16 * kKPitch, kVSize = 16 * kVPitch;
+constexpr int kKBufs = 3, kVBufs = 4;
+constexpr int kLevels = 1024;          // chunk levels of the longest-first order
+constexpr int kSorted = kPreThreads;   // prompts that are sorted, a thread each
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <int kFrom, int kTo, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (kFrom < kTo) {
+    f(std::integral_constant<int, kFrom>{});
+    each<kFrom + 1, kTo>(f);
+  }
+}
+
+// The first and a further MFMA of a score chain, with the scores in VGPRs and q
+// in AGPRs. As assembly, since the compiler would put every accumulator of this
+// kernel into AGPRs and copy the scores out of them, an instruction for each. It
+// does not know these as MFMAs, so what their hazards ask for is done by hand:
+// q is in place two instructions before the first (body), and no result is read
+// before 11 wait states after the last (body, and the scores' first use).
+__device__ __forceinline__ void mfma_first(f32x16& c, const bf16x8& a, const bf16x8& b) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "a"(b));
+}
+__device__ __forceinline__ void mfma_next(f32x16& c, const bf16x8& a, const bf16x8& b) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "a"(b));
+}
 
 // Rows [q0, q0 + n) of prompt b, clamped into the call's rows.
 struct Prompt {
@@ -28,37 +61,172 @@ __device__ __forceinline__ Prompt prompt_of(const PrefillArgs& a, int b, int* ba
   }
   return {q0, q1 - q0};
 }
+__device__ __forceinline__ int tiles_of(const PrefillArgs& a, int n) { return (n + a.tile_tokens - 1) / a.tile_tokens; }
 
-// Prompt b's tiles take places tile_base(b), tile_base(b) + 1, ...: a prompt of
-// n rows from row q0 on has at most (q0 + n) / tt + 1 - q0 / tt of them, so
-// places need no sum over the prompts.
-__device__ __forceinline__ int tile_base(const PrefillArgs& a, int b) {
-  const int q0 = min(max(a.indptr[(int64_t)b * a.indptr_s], 0), a.rows);
-  return q0 / a.tile_tokens + b;
+constexpr int kUnit = 1, kNoTile = 0, kEnd = -1;
+struct Plan {
+  int count[kLevels + 1];              // chunks of a level or above
+  int with[kLevels];                   // prompts that have a level
+  int4 chunks[kSorted / 4];            // chunks of each prompt
+  int sorted[kSorted];                 // prompts, those with most chunks first
+  int4 units[kPreThreads + 1];         // (first row of the prompt, its rows, tile, kUnit ..) of the workgroup's next units
+  int wave_tot[16];
+};
+
+// Inclusive sums from the end of a[0 .. kLevels), kLevels / kPreThreads entries a thread.
+__device__ __forceinline__ void suffix_sums(int* x, int* wave_tot) {
+  constexpr int kPer = kLevels / kPreThreads;
+  int v[kPer], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    v[i] = x[kLevels - 1 - (threadIdx.x * kPer + i)];
+    sum += v[i];
+  }
+  int total, before = block_exclusive_scan(sum, &total, wave_tot);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    before += v[i];
+    x[kLevels - 1 - (threadIdx.x * kPer + i)] = before;
+  }
+  __syncthreads();
 }
 
-// Whether a lane's part of O^T holds an infinity or a NaN (by the bits: device
-// code is compiled assuming no NaN operands).
-__device__ __forceinline__ bool odd_values(const f32x16 (&o)[4]) {
+// Longest first: chunks of 2^chunk_log neighbouring tiles by descending index
+// (level) in their prompt, which is their key range; within a level the prompts
+// with most chunks first, equal ones in order (every workgroup makes the same
+// plan). Two prefix sums over the levels give the place of every chunk: count[l]
+// of them have level l or above, and the prompts that have a level are the first
+// ones of `sorted`.
+__device__ __forceinline__ void plan_levels(const PrefillArgs& a, Plan& p, int* bad) {
+  const int tid = threadIdx.x;
+  for (int i = tid; i < kLevels; i += kPreThreads) p.with[i] = 0;
+  int mine = 0;
+  if (tid < a.B) mine = min(((tiles_of(a, prompt_of(a, tid, bad).n) - 1) >> a.chunk_log) + 1, kLevels);
+  reinterpret_cast<int*>(p.chunks)[tid] = mine;
+  __syncthreads();
+  if (mine > 0) atomicAdd(&p.with[mine - 1], 1);
+  int place = 0;
+  for (int i = 0; i < (a.B + 3) >> 2; ++i) {
+    const int4 c = p.chunks[i];
+    auto before = [&](int x, int b) { return x > mine || (x == mine && b < tid); };
+    place += before(c.x, 4 * i) + before(c.y, 4 * i + 1) + before(c.z, 4 * i + 2) + before(c.w, 4 * i + 3);
+  }
+  if (tid < a.B) p.sorted[place] = tid;
+  __syncthreads();
+  suffix_sums(p.with, p.wave_tot);
+  for (int i = tid; i < kLevels; i += kPreThreads) p.count[i] = p.with[i];
+  if (tid == 0) p.count[kLevels] = 0;
+  __syncthreads();
+  suffix_sums(p.count, p.wave_tot);
+}
+
+// The unit of rank `rank` of a head group.
+__device__ __forceinline__ int4 unit_of(const PrefillArgs& a, const Plan& p, int rank) {
+  int bad = 0, b, tile;
+  if (a.B <= kSorted) {
+    const int c = rank >> a.chunk_log;
+    if (c >= p.count[0]) return make_int4(0, 0, 0, kEnd);
+    int lo = 0;                          // the last level with count above c
+#pragma unroll
+    for (int step = kLevels / 2; step > 0; step >>= 1)
+      if (p.count[lo + step] > c) lo += step;
+    b = p.sorted[c - p.count[lo + 1]];
+    tile = (lo << a.chunk_log) + (1 << a.chunk_log) - 1 - (rank & ((1 << a.chunk_log) - 1));
+  } else {
+    // Too many prompts to sort (and no one of them is much of the call): in the
+    // order of the rows. Prompt b's tiles take the places from q0 / tt + b on,
+    // which are enough for them whatever the prompts' bounds, so no sum is needed.
+    const int places = a.rows / a.tile_tokens + a.B;
+    if (rank >= places) return make_int4(0, 0, 0, kEnd);
+    auto base = [&](int i) { return min(max(a.indptr[(int64_t)i * a.indptr_s], 0), a.rows) / a.tile_tokens + i; };
+    int lo = 0, hi = a.B - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (base(mid) <= rank) lo = mid; else hi = mid - 1;
+    }
+    b = lo;
+    tile = rank - base(b);
+  }
+  const Prompt x = prompt_of(a, b, &bad);
+  return make_int4(x.q0, x.n, tile, tile >= 0 && tile < tiles_of(a, x.n) ? kUnit : kNoTile);
+}
+
+// Whether a lane's part of O^T or of a row sum holds an infinity or a NaN (by the
+// bits: device code is compiled assuming no NaN operands).
+template <int NRB>
+__device__ __forceinline__ bool odd_values(const f32x16 (&o)[NRB][4], const float (&l)[NRB]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int jd = 0; jd < 4; ++jd)
+  for (int rb = 0; rb < NRB; ++rb) {
+    top = max(top, __float_as_uint(l[rb]) & 0x7fffffffu);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(o[jd][e]) & 0x7fffffffu);
+    for (int jd = 0; jd < 4; ++jd)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(o[rb][jd][e]) & 0x7fffffffu);
+  }
   return top >= 0x7f800000u;
 }
 
-// A masked key has probability 0, and 0 times an infinity or a NaN in its value
-// row is NaN: only such values bring one into a row that does not see them. So a
-// unit whose result holds one is computed again, with the tiles only up to the
-// first masked key and the others here, key by key, each for the rows that see it.
-__device__ __forceinline__ void attend_keys(const PrefillArgs& a, int q0, int g, int t0, int keys, int limit,
-                                            float sl2, const bf16x8 (&qv)[8], f32x16 (&o)[4], float& m, float& l) {
-  const int kg = (threadIdx.x & 63) >> 5;
+// A block of 32 rows of a unit (row r0 on) again, without the two shortcuts of the
+// fast path: the running maximum follows every step, and a masked key's value
+// takes no part at all (0 times an infinity or a NaN is NaN). By one wave, operands
+// straight from memory; keys below `whole`, which every row sees, by MFMA, the
+// others one by one. Not inlined: the fast path's registers are its own.
+typedef __attribute__((address_space(4))) const PrefillArgs ConstPrefillArgs;
+__device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int r0, int q0, int i0, int cnt, int g,
+                                                       int hb) {
+  const PrefillArgs a = *(const PrefillArgs*)ap;
+  const int lane = threadIdx.x & 63, col = lane & 31, kg = lane >> 5;
+  const int r = r0 + col, ti = r / a.rows_head, hr = r - ti * a.rows_head;
+  const bool ok = ti < cnt && hb * a.rows_head + hr < a.R;
+  const int head = g * a.R + hb * a.rows_head + (ok ? hr : 0);
+  const int64_t row = q0 + i0 + (ok ? ti : 0);
+  const int keys = i0 + cnt, limit = ok ? i0 + ti : keys - 1, whole = (i0 + 1) / 32 * 32;
+  const __bf16* kb = (const __bf16*)a.k + (int64_t)q0 * a.k_st + g * a.k_sh;
+  const __bf16* vb = (const __bf16*)a.v + (int64_t)q0 * a.v_st + g * a.v_sh;
+  bf16x8 qv[8];
+  load_q_operand((const __bf16*)a.q + row * a.q_st + (int64_t)head * a.q_sh, ok, qv);
+  const float sl2 = a.scale * kLog2e;
+  const f32x16 zero = {};
+  f32x16 o[4] = {zero, zero, zero, zero};
+  float m = kNoKey, l = 0.f;
 #pragma unroll 1
-  for (int t = t0; t < keys; ++t) {
-    const __bf16* kr = (const __bf16*)a.k + (int64_t)(q0 + t) * a.k_st + g * a.k_sh;
-    const __bf16* vr = (const __bf16*)a.v + (int64_t)(q0 + t) * a.v_st + g * a.v_sh + 4 * kg;
+  for (int t0 = 0; t0 < whole; t0 += 32) {
+    f32x16 s = zero;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      s = mfma_32x32x16(load_bf16x8(kb + (int64_t)(t0 + col) * a.k_st + 16 * c + 8 * kg), qv[c], s);
+    float mx = s[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    const float m_new = fmaxf(m, max_l32(mx) * sl2), alpha = exp2_fast(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int jd = 0; jd < 4; ++jd) o[jd] *= alpha;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = exp2_fast(fmaf(s[8 * h + e], sl2, -m));
+        l += x;
+        p[e] = (__bf16)x;
+      }
+#pragma unroll
+      for (int jd = 0; jd < 4; ++jd) {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          v[e] = vb[(int64_t)(t0 + 16 * h + 8 * (e >> 2) + 4 * kg + (e & 3)) * a.v_st + 32 * jd + col];
+        o[jd] = mfma_32x32x16(v, p, o[jd]);
+      }
+    }
+  }
+#pragma unroll 1
+  for (int t = whole; t < keys; ++t) {
+    const __bf16* kr = kb + (int64_t)t * a.k_st;
+    const __bf16* vr = vb + (int64_t)t * a.v_st + 4 * kg;
     float s = 0.f;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
@@ -77,116 +245,6 @@ __device__ __forceinline__ void attend_keys(const PrefillArgs& a, int q0, int g,
       for (int e = 0; e < 16; ++e)
         o[jd][e] = fmaf(p, (float)vr[32 * jd + 8 * (e >> 2) + (e & 3)], o[jd][e] * alpha);
   }
-}
-
-__global__ __launch_bounds__(kPreWaves * 64, 2) void prefill_kernel(PrefillArgs a) {
-  __shared__ u16 ks[kKeys][kKStride];
-  __shared__ u16 vs[kKeys][kVStride];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 31, kg = lane >> 5;
-  const int heads = a.Hkv * a.head_blocks;
-  const int place = blockIdx.x / heads, gh = blockIdx.x % heads;
-  const int g = gh / a.head_blocks, hb = gh % a.head_blocks;
-  int bad = 0;
-  if (gh == 0 && place < a.B) {          // (some workgroup checks each prompt's bounds)
-    prompt_of(a, place, &bad);
-    if (bad && tid == 0) atomicOr(a.err, bad);
-  }
-  int lo = 0, hi = a.B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (tile_base(a, mid) <= place) lo = mid; else hi = mid - 1;
-  }
-  const Prompt p = prompt_of(a, lo, &bad);
-  const int64_t i0_64 = (int64_t)(place - tile_base(a, lo)) * a.tile_tokens;
-  if (i0_64 < 0 || i0_64 >= p.n) return;
-  const int i0 = (int)i0_64;
-  const int cnt = min(a.tile_tokens, p.n - i0);
-  const int keys = i0 + cnt;             // keys [0, keys) are visible to some row, [0, i0] to every row
-
-  const int RB = a.rows_head, r = wave * kWaveRows + col;
-  const int ti = r / RB, hr = r - ti * RB;
-  const bool ok = ti < cnt && hb * RB + hr < a.R;
-  const int limit = ok ? i0 + ti : keys - 1;
-  const int64_t row = p.q0 + i0 + (ok ? ti : 0);
-  const int head = g * a.R + hb * RB + (ok ? hr : 0);
-  bf16x8 qv[8];
-  load_q_operand((const __bf16*)a.q + row * a.q_st + (int64_t)head * a.q_sh, ok, qv);
-  const float sl2 = a.scale * kLog2e;
-  f32x16 o[4];
-  float m, l;
-  const int ld_row = tid >> 4, ld_chunk = (tid & 15) * 8;
-  const int tr_row = 4 * kg + ((lane & 15) >> 2);
-  const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  auto attend = [&](int t_end) {
-#pragma unroll
-  for (int jd = 0; jd < 4; ++jd)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[jd][e] = 0.f;
-  m = kNoKey;
-  l = 0.f;
-  for (int t0 = 0; t0 < t_end; t0 += kKeys) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int t = min(t0 + ld_row + 32 * i, keys - 1);
-      const int64_t kr = p.q0 + t;
-      *reinterpret_cast<bf16x8*>(&ks[ld_row + 32 * i][ld_chunk]) =
-          load_bf16x8((const __bf16*)a.k + kr * a.k_st + g * a.k_sh + ld_chunk);
-      *reinterpret_cast<bf16x8*>(&vs[ld_row + 32 * i][ld_chunk]) =
-          load_bf16x8((const __bf16*)a.v + kr * a.v_st + g * a.v_sh + ld_chunk);
-    }
-    __syncthreads();
-    f32x16 sc[2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[kb][e] = 0.f;
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        sc[kb] = mfma_32x32x16(*reinterpret_cast<const bf16x8*>(&ks[32 * kb + col][16 * c + 8 * kg]), qv[c], sc[kb]);
-    }
-    float mt = kNegInf;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        if (t0 + 32 * kb + 8 * (e >> 2) + 4 * kg + (e & 3) > limit) sc[kb][e] = kNegInf;
-        mt = fmaxf(mt, sc[kb][e]);
-      }
-    const float m_new = fmaxf(m, max_l32(mt) * sl2);
-    const float alpha = exp2_fast(m - m_new);
-    m = m_new;
-    l *= alpha;
-#pragma unroll
-    for (int jd = 0; jd < 4; ++jd) o[jd] *= alpha;
-    bf16x8 pb[4];
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = exp2_fast(fmaf(sc[h >> 1][8 * (h & 1) + e], sl2, -m));
-        l += x;
-        pb[h][e] = (__bf16)x;
-      }
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-#pragma unroll
-      for (int jd = 0; jd < 4; ++jd) {
-        const u16* vp = &vs[16 * h + tr_row][32 * jd + tr_col];
-        const i16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)vp);
-        const i16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vp + 8 * kVStride));
-        const i16x8 v8 = __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
-        o[jd] = mfma_32x32x16(__builtin_bit_cast(bf16x8, v8), pb[h], o[jd]);
-      }
-  }
-  };
-  attend(keys);
-  if (__syncthreads_or(odd_values(o))) {
-    const int whole = (i0 + 1) / kKeys * kKeys;
-    attend(whole);
-    attend_keys(a, p.q0, g, whole, keys, limit, sl2, qv, o, m, l);
-  }
   const float l_tot = sum_l32(l);
   if (!ok) return;
   const float inv = 1.f / l_tot;
@@ -198,13 +256,395 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void prefill_kernel(PrefillArgs 
     a.lse[row * a.lse_st + (int64_t)head * a.lse_sh] = (m + __builtin_amdgcn_logf(l_tot)) * kLn2;
 }
 
+template <int NRB>
+__global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) {
+  __shared__ __attribute__((aligned(16))) char kl[kKBufs * kKSize], vl[kVBufs * kVSize];
+  __shared__ Plan plan;
+  constexpr int kSlots = 32 * NRB;                 // MFMAs of a step
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, kg = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int heads = a.Hkv * a.head_blocks, gh = blockIdx.x % heads;
+  const int g = gh / a.head_blocks, hb = gh % a.head_blocks;
+  const int w = blockIdx.x / heads, ws = gridDim.x / heads;   // workgroups of this head group
+  const float sl2 = a.scale * kLog2e;
+  int bad = 0;
+  if (a.B <= kSorted) {
+    plan_levels(a, plan, &bad);
+    if (blockIdx.x != 0) bad = 0;                  // (the first workgroup reports the prompts' bounds)
+  } else {
+    for (int b = blockIdx.x * kPreThreads + tid; b < a.B; b += gridDim.x * kPreThreads) prompt_of(a, b, &bad);
+  }
+  if (bad) atomicOr(a.err, bad);
+
+  // rows of a step go from memory to LDS by the load itself: block b of 16 holds
+  // rows b + 16 s (s = lane / 16), wave w fills blocks 4 w .. 4 w + 3
+  const uint32_t kss = 2u * (uint32_t)a.k_st, vss = 2u * (uint32_t)a.v_st;
+  const int lrow = 16 * (lane >> 4) + 4 * wave;
+  const uint32_t lchunk = 16u * (lane & 15);
+  uint32_t kvo[4], vvo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    kvo[i] = (uint32_t)(lrow + i) * kss + lchunk;
+    vvo[i] = (uint32_t)(lrow + i) * vss + lchunk;
+  }
+  auto load_step = [&](const char* rows, uint32_t ss, const uint32_t (&vo)[4], char* dst, int pitch, int last) {
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(dst + 4 * wave * pitch);
+    // (as assembly: see the 128-key routine in tile_attn.hpp. m0, the LDS address, is an input that the compiler sets)
+    if (last >= kStep - 1) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(vo[i]), "s"(rows), "{m0}"(lds + i * pitch) : "memory");
+    } else {                                       // rows past the last key load that key again
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"((uint32_t)min(lrow + i, last) * ss + lchunk), "s"(rows),
+                     "{m0}"(lds + i * pitch) : "memory");
+    }
+  };
+  auto barrier = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto after = [&](int x, int size, int bufs) { return x + size == bufs * size ? 0 : x + size; };
+
+  struct Unit {
+    int q0, i0, cnt, keys;
+    const char *k, *v;
+  };
+  auto unit_at = [&](int i) {
+    const int4 x = plan.units[i];
+    Unit u;
+    u.q0 = __builtin_amdgcn_readfirstlane(x.x);
+    const int n = __builtin_amdgcn_readfirstlane(x.y);
+    u.i0 = __builtin_amdgcn_readfirstlane(x.z) * a.tile_tokens;
+    u.cnt = min(a.tile_tokens, n - u.i0);
+    u.keys = u.i0 + u.cnt;                         // keys [0, keys) are visible to some row, [0, i0] to every row
+    u.k = (const char*)((const __bf16*)a.k + (int64_t)u.q0 * a.k_st + g * a.k_sh);
+    u.v = (const char*)((const __bf16*)a.v + (int64_t)u.q0 * a.v_st + g * a.v_sh);
+    return u;
+  };
+  struct Row {
+    bool ok;
+    int ti, head;
+    int64_t row;
+  };
+  auto row_of = [&](const Unit& u, int thread, int rb) {
+    const int r = (thread >> 6) * (32 * NRB) + 32 * rb + (thread & 31);
+    const int ti = r / a.rows_head, hr = r - ti * a.rows_head;
+    const bool ok = ti < u.cnt && hb * a.rows_head + hr < a.R;
+    return Row{ok, ti, g * a.R + hb * a.rows_head + (ok ? hr : 0), (int64_t)(u.q0 + u.i0 + (ok ? ti : 0))};
+  };
+  auto q_at = [&](const Row& r) { return (const __bf16*)a.q + r.row * a.q_st + (int64_t)r.head * a.q_sh; };
+
+  bf16x8 qv[NRB][8];
+  int k0 = 0, v0 = 0;                              // buffers of a unit's first step
+  // what a unit needs before its first step
+  auto request = [&](const Unit& u, int kb, int vb) {
+    const int last = u.keys - 1;
+    load_step(u.k, kss, kvo, kl + kb, kKPitch, last);
+    if (last >= kStep) load_step(u.k + kStep * (int64_t)kss, kss, kvo, kl + after(kb, kKSize, kKBufs), kKPitch, last - kStep);
+    load_step(u.v, vss, vvo, vl + vb, kVPitch, last);
+    if (last >= 2 * kStep)
+      load_step(u.k + 2 * kStep * (int64_t)kss, kss, kvo, kl + after(after(kb, kKSize, kKBufs), kKSize, kKBufs), kKPitch,
+                last - 2 * kStep);
+    if (last >= kStep) load_step(u.v + kStep * (int64_t)vss, vss, vvo, vl + after(vb, kVSize, kVBufs), kVPitch, last - kStep);
+    int t = tid;
+    asm volatile("" : "+v"(t));
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      const Row r = row_of(u, t, rb);
+      load_q_operand(q_at(r), r.ok, qv[rb]);
+    }
+  };
+
+  const int kread = (col & 15) * kKPitch + (col >> 4) * 256 + 16 * kg;
+  const int tr_row = 4 * kg + ((lane & 15) >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  const int vread = tr_row * kVPitch + 2 * tr_col;
+  // operand i of an iteration: 0 .. 15 of V (16 keys i / 4, 32 dimensions i % 4), 16 .. 31 of K (32 keys, 16 dimensions)
+  auto read = [&](auto i_, const char* vb, const char* kb) -> bf16x8 {
+    constexpr int i = decltype(i_)::value;
+    if constexpr (i < 16) {
+      const char* vp = vb + 256 * (i >> 2) + 64 * (i & 3);
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)vp);
+      const i16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vp + 8 * kVPitch));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      return *reinterpret_cast<const bf16x8*>(kb + 512 * ((i - 16) >> 3) + 32 * (i & 7));
+    }
+  };
+  const std::true_type yes{};
+  const std::false_type no{};
+
+  for (int base = 0;; base += kPreThreads) {
+    // this workgroup's next units: every second round in opposite order, so that the sums of a longest-first list even out
+    __syncthreads();
+    {
+      const int k = base + tid;
+      plan.units[tid] = unit_of(a, plan, k * ws + ((k & 1) ? ws - 1 - w : w));
+      if (tid == 0) plan.units[kPreThreads] = make_int4(0, 0, 0, kNoTile);
+    }
+    __syncthreads();
+    auto next_of = [&](int i) {                    // the next entry that is a unit; kPreThreads if none
+      while (i < kPreThreads && __builtin_amdgcn_readfirstlane(plan.units[i].w) == kNoTile) ++i;
+      return i;
+    };
+    int at = next_of(0);
+    if (at < kPreThreads && __builtin_amdgcn_readfirstlane(plan.units[at].w) == kEnd) break;
+    if (at == kPreThreads) continue;
+    Unit u = unit_at(at);
+    request(u, k0, v0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    bool end = false;
+    for (;;) {
+      at = next_of(at + 1);
+      end = at < kPreThreads && __builtin_amdgcn_readfirstlane(plan.units[at].w) == kEnd;
+      const bool more = at < kPreThreads && !end;
+      Unit un = u;
+      if (more) un = unit_at(at);
+      const int n = (u.keys + kStep - 1) / kStep;
+      const int n_full = (u.i0 + 1) / kStep;       // steps [0, n_full) need no mask
+      int limit[NRB];
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) {
+        const Row r = row_of(u, tid, rb);
+        limit[rb] = r.ok ? u.i0 + r.ti : u.keys - 1;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) asm volatile("" : "+a"(qv[rb][c]));
+      }
+      barrier();                                   // the first steps' rows are in LDS
+      const f32x16 zero = {};
+      f32x16 o[NRB][4], s[2][NRB];                 // O^T, and S^T(j) of the current step [32 keys][row block]
+      bf16x8 pb[NRB][4];                           // P^T(j - 1)
+      bf16x8 ring[kRing];
+      float nm[NRB], l[NRB], l2[NRB];              // minus the maximum, and two sums
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) {
+        l[rb] = l2[rb] = 0.f;
+#pragma unroll
+        for (int jd = 0; jd < 4; ++jd) o[rb][jd] = zero;
+      }
+      {
+        const char* kb = kl + k0 + kread;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const bf16x8 x = *reinterpret_cast<const bf16x8*>(kb + 512 * b + 32 * c);
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) s[b][rb] = mfma_32x32x16(x, qv[rb][c], c == 0 ? zero : s[b][rb]);
+          }
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+          float mx = kNegInf;
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              mx = fmaxf(mx, 32 * b + 8 * (e >> 2) + 4 * kg + (e & 3) <= limit[rb] ? s[b][rb][e] : kNegInf);
+          nm[rb] = -max_l32(mx) * sl2;
+        }
+      }
+      barrier();                                   // K(0)'s buffer is free
+      // buffers of V(j - 1), V(j), V(j + 2), K(j + 1), K(j + 3), and the rows that come next
+      int v_prev = 0, v_cur = v0, v_next2 = after(after(v0, kVSize, kVBufs), kVSize, kVBufs);
+      int k_next = after(k0, kKSize, kKBufs), k_next3 = k0;
+      const char* kp = u.k + 3 * kStep * (int64_t)kss;
+      const char* vp = u.v + 2 * kStep * (int64_t)vss;
+      // iteration j: the values of step j - 1, the softmax of step j, the scores of step j + 1
+      auto body = [&](int j, auto pv_tag, auto s_tag, auto mask_tag) {
+        constexpr bool kPV = decltype(pv_tag)::value, kS = decltype(s_tag)::value, kMask = decltype(mask_tag)::value;
+        const char* vb = vl + v_prev + vread;
+        const char* vb_next = vl + v_cur + vread;
+        const char* kb = kl + k_next + kread;
+        f32x16 sn[2][NRB];
+        u32x4 pn[NRB][4];
+        float t1, p0, p1, q0, q1;
+        const int d0 = u.keys - 1 - j * kStep - 4 * kg;
+        auto finish = [&](auto x_, int part) {     // sums and conversion of pair x
+          constexpr int x = decltype(x_)::value;
+          if constexpr (x >= 0) {
+            constexpr int h = x / (4 * NRB), rb = (x >> 2) % NRB, e = x & 3;
+            if (part == 0) {
+              l[rb] += q0;
+            } else {
+              l2[rb] += q1;
+              uint32_t w2 = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)q0, (__bf16)q1});
+              asm volatile("" : "+v"(w2));
+              pn[rb][h][e] = w2;
+            }
+          }
+        };
+        auto soft = [&](auto slot_) {
+          constexpr int slot = decltype(slot_)::value, x = slot >> 1;
+          constexpr int h = x / (4 * NRB), rb = (x >> 2) % NRB, e = 2 * (x & 3);
+          if constexpr ((slot & 1) == 0) {
+            float t0 = fmaf(s[h >> 1][rb][8 * (h & 1) + e], sl2, nm[rb]);
+            t1 = fmaf(s[h >> 1][rb][8 * (h & 1) + e + 1], sl2, nm[rb]);
+            if constexpr (kMask) {
+              constexpr int z = 8 * (h & 1) + e, key = 32 * (h >> 1) + 8 * (z >> 2) + (z & 3);
+              const int d = min(limit[rb] - j * kStep - 4 * kg, d0);
+              if (key > d) t0 = kNegInf;
+              if (key + 1 > d) t1 = kNegInf;
+            }
+            q0 = p0;
+            q1 = p1;
+            p0 = exp2_fast(t0);
+            finish(std::integral_constant<int, x - 1>{}, 0);
+          } else {
+            p1 = exp2_fast(t1);
+            finish(std::integral_constant<int, x - 1>{}, 1);
+          }
+        };
+        if constexpr (kS) {
+          if (j + 2 < n) load_step(vp, vss, vvo, vl + v_next2, kVPitch, u.keys - 1 - (j + 2) * kStep);
+          if (j + 3 < n) load_step(kp, kss, kvo, kl + k_next3, kKPitch, u.keys - 1 - (j + 3) * kStep);
+          vp += kStep * (int64_t)vss;
+          kp += kStep * (int64_t)kss;
+          asm volatile("s_nop 1" ::"a"(qv[0][0]), "a"(qv[0][1]), "a"(qv[0][2]), "a"(qv[0][3]), "a"(qv[0][4]),
+                       "a"(qv[0][5]), "a"(qv[0][6]), "a"(qv[0][7]));
+          if constexpr (NRB == 2)
+            asm volatile("s_nop 1" ::"a"(qv[NRB - 1][0]), "a"(qv[NRB - 1][1]), "a"(qv[NRB - 1][2]), "a"(qv[NRB - 1][3]),
+                         "a"(qv[NRB - 1][4]), "a"(qv[NRB - 1][5]), "a"(qv[NRB - 1][6]), "a"(qv[NRB - 1][7]));
+          __builtin_amdgcn_sched_barrier(0);
+        } else if (more) {
+          request(un, k_next, after(v_cur, kVSize, kVBufs));
+        }
+        constexpr int i0 = kPV ? 0 : 16, i1 = kS ? 32 : 16;
+        if constexpr (!kPV && kS) each<16, 16 + kAhead>([&](auto i) { ring[i % kRing] = read(i, vb, kb); });
+        if constexpr (!kPV) each<0, kSlots / 2>([&](auto i) { soft(i); });
+        each<i0, i1>([&](auto i) {
+          // (behind the last, the first of the next iteration: values of step j)
+          if constexpr (i + kAhead < i1)
+            ring[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead>{}, vb, kb);
+          else
+            ring[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead - i1>{}, vb_next, kb);
+          __builtin_amdgcn_sched_barrier(0);
+          each<0, NRB>([&](auto rb) {
+            if constexpr (i < 16)
+              o[rb][i & 3] = mfma_32x32x16(ring[i % kRing], pb[rb][i >> 2], o[rb][i & 3]);
+            else if constexpr ((i & 7) == 0)
+              mfma_first(sn[(i - 16) >> 3][rb], ring[i % kRing], qv[rb][0]);
+            else
+              mfma_next(sn[(i - 16) >> 3][rb], ring[i % kRing], qv[rb][i & 7]);
+            __builtin_amdgcn_sched_barrier(0);
+            soft(std::integral_constant<int, NRB * i + rb>{});
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        });
+        if constexpr (!kS) each<kSlots / 2, kSlots>([&](auto i) { soft(i); });
+        q0 = p0;
+        q1 = p1;
+        finish(std::integral_constant<int, kSlots / 2 - 1>{}, 0);
+        finish(std::integral_constant<int, kSlots / 2 - 1>{}, 1);
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) asm volatile("" : "+v"(l[rb]), "+v"(l2[rb]));
+        if constexpr (i0 == i1) each<0, kAhead>([&](auto i) { ring[i] = read(i, vb_next, kb); });
+        if constexpr (kS) asm volatile("s_nop 11" ::: "memory");   // S^T(j + 1) is complete
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+          for (int h = 0; h < 4; ++h) pb[rb][h] = __builtin_bit_cast(bf16x8, pn[rb][h]);
+        if constexpr (kS) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int rb = 0; rb < NRB; ++rb) s[b][rb] = sn[b][rb];
+        }
+      };
+      auto turn = [&](int j) {
+        // the rows of V(j + 1) and K(j + 2), requested an iteration ago, have come
+        if (j + 3 < n)
+          asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        else
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        barrier();
+        v_prev = v_cur;
+        v_cur = after(v_cur, kVSize, kVBufs);
+        v_next2 = after(v_next2, kVSize, kVBufs);
+        k_next = after(k_next, kKSize, kKBufs);
+        k_next3 = after(k_next3, kKSize, kKBufs);
+      };
+      if (n == 1) {
+        body(0, no, no, yes);
+      } else {
+        if (n_full > 0)
+          body(0, no, yes, no);
+        else
+          body(0, no, yes, yes);
+        turn(0);
+        int j = 1;
+        for (; j + 1 < n && j < n_full; ++j) {
+          body(j, yes, yes, no);
+          turn(j);
+        }
+        for (; j + 1 < n; ++j) {
+          body(j, yes, yes, yes);
+          turn(j);
+        }
+        body(j, yes, no, yes);
+      }
+      // the values of the last step (its first operands are read)
+      {
+        const char* vb = vl + v_cur + vread;
+        each<0, 16>([&](auto i) {
+          if constexpr (i + kAhead < 16)
+            ring[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead>{}, vb, vb);
+#pragma unroll
+          for (int rb = 0; rb < NRB; ++rb)
+            o[rb][i & 3] = mfma_32x32x16(ring[i % kRing], pb[rb][i >> 2], o[rb][i & 3]);
+        });
+      }
+      k0 = k_next;
+      v0 = after(v_cur, kVSize, kVBufs);
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) l[rb] += l2[rb];
+      // (formed again: kept over the loop they would cost registers)
+      int t = tid;
+      asm volatile("" : "+v"(t));
+      const bool again = __builtin_amdgcn_ballot_w64(odd_values<NRB>(o, l)) != 0;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the next unit's rows have come (before the stores, which need not)
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) {
+        const float l_tot = sum_l32(l[rb]);
+        const Row r = row_of(u, t, rb);
+        if (!r.ok || again) continue;
+        const float inv = 1.f / l_tot;
+        if (a.out_f32)
+          store_o_row((float*)a.out + r.row * a.out_st + (int64_t)r.head * a.out_sh, o[rb], inv);
+        else
+          store_o_row((__bf16*)a.out + r.row * a.out_st + (int64_t)r.head * a.out_sh, o[rb], inv);
+        if (a.lse && (t & 63) < 32)
+          a.lse[r.row * a.lse_st + (int64_t)r.head * a.lse_sh] = (__builtin_amdgcn_logf(l_tot) - nm[rb]) * kLn2;
+      }
+      if (again) {
+        for (int rb = 0; rb < NRB; ++rb)
+          attend_again((ConstPrefillArgs*)__builtin_amdgcn_kernarg_segment_ptr(), wave * (32 * NRB) + 32 * rb, u.q0, u.i0,
+                       u.cnt, g, hb);
+      }
+      if (!more) break;
+      u = un;
+    }
+    if (end) break;
+  }
+}
+
 }  // namespace
 
-hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream, KernelTimer* timer) {
-  const int64_t places = a.rows / a.tile_tokens + a.B;
-  const unsigned grid = (unsigned)(places * a.Hkv * a.head_blocks);
+hipError_t launch_prefill(const PrefillArgs& args, int cus, hipStream_t stream, KernelTimer* timer) {
+  PrefillArgs a = args;
+  const int64_t tiles = a.rows / a.tile_tokens;
+  a.chunk_log = a.rows / a.B >= 16 * a.tile_tokens ? 2 : 0;
+  while ((tiles >> a.chunk_log) + 1 > kLevels) ++a.chunk_log;
+  const int64_t heads = (int64_t)a.Hkv * a.head_blocks;
+  const int64_t most = tiles + ((int64_t)a.B << a.chunk_log);    // ranks of a head group, at most
+  const unsigned grid = (unsigned)(heads * std::max<int64_t>(1, std::min<int64_t>(cus / heads, most)));
   if (timer) (void)hipEventRecord(timer->start, stream);
-  prefill_kernel<<<grid, kPreWaves * 64, 0, stream>>>(a);
+  if (a.tile_rows == 256)
+    prefill_kernel<2><<<grid, kPreThreads, 0, stream>>>(a);
+  else
+    prefill_kernel<1><<<grid, kPreThreads, 0, stream>>>(a);
   if (timer) (void)hipEventRecord(timer->stop, stream);
   return hipGetLastError();
 }

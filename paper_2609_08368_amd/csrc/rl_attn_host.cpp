@@ -550,10 +550,10 @@ struct ExtendShape {
 // query rows per extend work unit: eight waves of 32 rows
 constexpr int kExtendRows = 256;
 
-ExtendShape extend_shape(int64_t R) {
+ExtendShape extend_shape(int64_t R, int rows = kExtendRows) {
   ExtendShape s;
-  s.rows_head = (int)std::min<int64_t>(R, kExtendRows);
-  s.tile_tokens = std::max(1, kExtendRows / s.rows_head);
+  s.rows_head = (int)std::min<int64_t>(R, rows);
+  s.tile_tokens = std::max(1, rows / s.rows_head);
   s.head_blocks = (int)((R + s.rows_head - 1) / s.rows_head);
   return s;
 }
@@ -1252,13 +1252,18 @@ int prefill_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, con
   RL_TRY(check_data(q, "q"));
   if (B == 0 || rows == 0) return RL_OK;
   rl::PrefillArgs a{};
-  const ExtendShape s = extend_shape(Hq / Hkv);
+  int cus = 0;
+  RL_TRY(current_cus(&cus));
+  // tiles of 128 rows where those of 256 would leave CUs idle (see the kernel)
+  const int64_t R = Hq / Hkv;
+  auto units = [&](const ExtendShape& x) { return (rows / x.tile_tokens + B) * Hkv * x.head_blocks; };
+  a.tile_rows = units(extend_shape(R)) < cus ? 128 : 256;
+  const ExtendShape s = extend_shape(R, a.tile_rows);
   a.rows_head = s.rows_head;
   a.tile_tokens = s.tile_tokens;
   a.head_blocks = s.head_blocks;
-  // (a launch has fewer than 2^32 threads)
-  if ((rows / a.tile_tokens + B) * Hkv * a.head_blocks >= (1 << 23))
-    return fail(RL_ERR_UNSUPPORTED, "rows times heads too large");
+  // (ranks of units and places of tiles are 32-bit)
+  if (rows / a.tile_tokens + 32 * B > INT32_MAX) return fail(RL_ERR_UNSUPPORTED, "rows or batch too large");
   hipStream_t st = static_cast<hipStream_t>(stream);
   Workspace* w = nullptr;
   RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
@@ -1289,7 +1294,7 @@ int prefill_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, con
   a.err = w->err;
   rl::KernelTimer slot;
   rl::KernelTimer* timer = prof_timer(&slot, st);
-  const hipError_t e = rl::launch_prefill(a, st, timer);
+  const hipError_t e = rl::launch_prefill(a, cus, st, timer);
   prof_commit(3, timer);
   if (e != hipSuccess) return hip_fail(e, "prefill kernel launch");
   return RL_OK;
