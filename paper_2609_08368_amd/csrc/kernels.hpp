@@ -300,6 +300,7 @@ struct PrefillArgs {
   int B, rows, Hq, Hkv, R;
   int tile_rows;          // query rows per tile: 128 or 256
   int rows_head;          // query heads per tile
+  float rows_head_inv;
   int tile_tokens;        // prompt tokens per tile
   int head_blocks;        // ceil(R / rows_head)
   int chunk_log;          // log2 of the tiles that are neighbours in the order of the units

@@ -68,7 +68,7 @@ struct Plan {
   int count[kLevels + 1];              // chunks of a level or above
   int with[kLevels];                   // prompts that have a level
   int4 chunks[kSorted / 4];            // chunks of each prompt
-  int sorted[kSorted];                 // prompts, those with most chunks first
+  int2 sorted[kSorted];                // (first row, rows) of the prompts, those with most chunks first
   int4 units[kPreThreads + 1];         // (first row of the prompt, its rows, tile, kUnit ..) of the workgroup's next units
   int wave_tot[16];
 };
@@ -99,9 +99,20 @@ __device__ __forceinline__ void suffix_sums(int* x, int* wave_tot) {
 // ones of `sorted`.
 __device__ __forceinline__ void plan_levels(const PrefillArgs& a, Plan& p, int* bad) {
   const int tid = threadIdx.x;
+  if (a.B == 1) {
+    if (tid == 0) {
+      const Prompt x = prompt_of(a, 0, bad);
+      p.sorted[0] = make_int2(x.q0, x.n);
+    }
+    return;                              // (the caller synchronises)
+  }
   for (int i = tid; i < kLevels; i += kPreThreads) p.with[i] = 0;
   int mine = 0;
-  if (tid < a.B) mine = min(((tiles_of(a, prompt_of(a, tid, bad).n) - 1) >> a.chunk_log) + 1, kLevels);
+  Prompt x{0, 0};
+  if (tid < a.B) {
+    x = prompt_of(a, tid, bad);
+    mine = min(((tiles_of(a, x.n) - 1) >> a.chunk_log) + 1, kLevels);
+  }
   reinterpret_cast<int*>(p.chunks)[tid] = mine;
   __syncthreads();
   if (mine > 0) atomicAdd(&p.with[mine - 1], 1);
@@ -111,7 +122,7 @@ __device__ __forceinline__ void plan_levels(const PrefillArgs& a, Plan& p, int* 
     auto before = [&](int x, int b) { return x > mine || (x == mine && b < tid); };
     place += before(c.x, 4 * i) + before(c.y, 4 * i + 1) + before(c.z, 4 * i + 2) + before(c.w, 4 * i + 3);
   }
-  if (tid < a.B) p.sorted[place] = tid;
+  if (tid < a.B) p.sorted[place] = make_int2(x.q0, x.n);
   __syncthreads();
   suffix_sums(p.with, p.wave_tot);
   for (int i = tid; i < kLevels; i += kPreThreads) p.count[i] = p.with[i];
@@ -122,16 +133,26 @@ __device__ __forceinline__ void plan_levels(const PrefillArgs& a, Plan& p, int* 
 
 // The unit of rank `rank` of a head group.
 __device__ __forceinline__ int4 unit_of(const PrefillArgs& a, const Plan& p, int rank) {
-  int bad = 0, b, tile;
+  int bad = 0, tile;
+  Prompt x;
   if (a.B <= kSorted) {
     const int c = rank >> a.chunk_log;
-    if (c >= p.count[0]) return make_int4(0, 0, 0, kEnd);
-    int lo = 0;                          // the last level with count above c
+    int level, k = 0;
+    if (a.B == 1) {                      // (a lone prompt needs no sums)
+      const int2 y = p.sorted[0];
+      level = ((tiles_of(a, y.y) - 1) >> a.chunk_log) - c;
+      if (level < 0 || y.y == 0) return make_int4(0, 0, 0, kEnd);
+    } else {
+      if (c >= p.count[0]) return make_int4(0, 0, 0, kEnd);
+      level = 0;                         // the last level with count above c
 #pragma unroll
-    for (int step = kLevels / 2; step > 0; step >>= 1)
-      if (p.count[lo + step] > c) lo += step;
-    b = p.sorted[c - p.count[lo + 1]];
-    tile = (lo << a.chunk_log) + (1 << a.chunk_log) - 1 - (rank & ((1 << a.chunk_log) - 1));
+      for (int step = kLevels / 2; step > 0; step >>= 1)
+        if (p.count[level + step] > c) level += step;
+      k = c - p.count[level + 1];
+    }
+    const int2 y = p.sorted[k];
+    x = {y.x, y.y};
+    tile = (level << a.chunk_log) + (1 << a.chunk_log) - 1 - (rank & ((1 << a.chunk_log) - 1));
   } else {
     // Too many prompts to sort (and no one of them is much of the call): in the
     // order of the rows. Prompt b's tiles take the places from q0 / tt + b on,
@@ -144,10 +165,9 @@ __device__ __forceinline__ int4 unit_of(const PrefillArgs& a, const Plan& p, int
       const int mid = (lo + hi + 1) >> 1;
       if (base(mid) <= rank) lo = mid; else hi = mid - 1;
     }
-    b = lo;
-    tile = rank - base(b);
+    tile = rank - base(lo);
+    x = prompt_of(a, lo, &bad);
   }
-  const Prompt x = prompt_of(a, b, &bad);
   return make_int4(x.q0, x.n, tile, tile >= 0 && tile < tiles_of(a, x.n) ? kUnit : kNoTile);
 }
 
@@ -256,9 +276,44 @@ __device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int
     a.lse[row * a.lse_st + (int64_t)head * a.lse_sh] = (m + __builtin_amdgcn_logf(l_tot)) * kLn2;
 }
 
+// A wave's 32 rows to memory. O^T has a row's dimensions in two lanes, four
+// neighbours at a time, so stores from there would touch 32 rows each with 16
+// bytes (which took 9,000 cycles a unit: an instruction costs a cycle or two per
+// line); through LDS (wave-private, 128 bytes of each row at once) an
+// instruction writes whole lines of eight rows. row(i, ok): address of row i.
+constexpr int kOutPitch = 128 + 16;
+template <typename T, typename RowOf>
+__device__ __forceinline__ void store_block(const f32x16 (&o)[4], float inv, char* lds, RowOf&& row) {
+  constexpr int kJd = 4 / sizeof(T);               // 32-dimension blocks in 128 bytes
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63, col = lane & 31, kg = lane >> 5;
+  T* to[4];
+  bool ok[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) to[i] = row(8 * i + (lane >> 3), &ok[i]);
+#pragma unroll
+  for (int part = 0; part < 4 / kJd; ++part) {
+#pragma unroll
+    for (int jd = 0; jd < kJd; ++jd)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        t4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (T)(o[part * kJd + jd][4 * q + i] * inv);
+        *reinterpret_cast<t4*>(lds + col * kOutPitch + (32 * jd + 8 * q + 4 * kg) * (int)sizeof(T)) = x;
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(lds + (8 * i + (lane >> 3)) * kOutPitch + 16 * (lane & 7));
+      if (ok[i]) *reinterpret_cast<u32x4*>(to[i] + 32 * kJd * part + (16 / (int)sizeof(T)) * (lane & 7)) = x;
+    }
+  }
+}
+
 template <int NRB>
 __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) {
   __shared__ __attribute__((aligned(16))) char kl[kKBufs * kKSize], vl[kVBufs * kVSize];
+  __shared__ __attribute__((aligned(16))) char outl[4][32 * kOutPitch];
   __shared__ Plan plan;
   constexpr int kSlots = 32 * NRB;                 // MFMAs of a step
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, kg = lane >> 5;
@@ -331,7 +386,8 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
   };
   auto row_of = [&](const Unit& u, int thread, int rb) {
     const int r = (thread >> 6) * (32 * NRB) + 32 * rb + (thread & 31);
-    const int ti = r / a.rows_head, hr = r - ti * a.rows_head;
+    // r / rows_head for r < 256: r + 1/2 is at least 2^-9 of it away from a multiple
+    const int ti = (int)(((float)r + 0.5f) * a.rows_head_inv), hr = r - ti * a.rows_head;
     const bool ok = ti < u.cnt && hb * a.rows_head + hr < a.R;
     return Row{ok, ti, g * a.R + hb * a.rows_head + (ok ? hr : 0), (int64_t)(u.q0 + u.i0 + (ok ? ti : 0))};
   };
@@ -609,13 +665,18 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
       for (int rb = 0; rb < NRB; ++rb) {
         const float l_tot = sum_l32(l[rb]);
         const Row r = row_of(u, t, rb);
-        if (!r.ok || again) continue;
+        if (again) continue;
         const float inv = 1.f / l_tot;
+        auto row = [&](auto* out, int i, bool* ok) {
+          const Row x = row_of(u, (t & ~63) + i, rb);
+          *ok = x.ok;
+          return out + x.row * a.out_st + (int64_t)x.head * a.out_sh;
+        };
         if (a.out_f32)
-          store_o_row((float*)a.out + r.row * a.out_st + (int64_t)r.head * a.out_sh, o[rb], inv);
+          store_block<float>(o[rb], inv, outl[wave], [&](int i, bool* ok) { return row((float*)a.out, i, ok); });
         else
-          store_o_row((__bf16*)a.out + r.row * a.out_st + (int64_t)r.head * a.out_sh, o[rb], inv);
-        if (a.lse && (t & 63) < 32)
+          store_block<__bf16>(o[rb], inv, outl[wave], [&](int i, bool* ok) { return row((__bf16*)a.out, i, ok); });
+        if (a.lse && r.ok && (t & 63) < 32)
           a.lse[r.row * a.lse_st + (int64_t)r.head * a.lse_sh] = (__builtin_amdgcn_logf(l_tot) - nm[rb]) * kLn2;
       }
       if (again) {
@@ -640,6 +701,7 @@ hipError_t launch_prefill(const PrefillArgs& args, int cus, hipStream_t stream, 
   const int64_t heads = (int64_t)a.Hkv * a.head_blocks;
   const int64_t most = tiles + ((int64_t)a.B << a.chunk_log);    // ranks of a head group, at most
   const unsigned grid = (unsigned)(heads * std::max<int64_t>(1, std::min<int64_t>(cus / heads, most)));
+  a.rows_head_inv = 1.f / (float)a.rows_head;
   if (timer) (void)hipEventRecord(timer->start, stream);
   if (a.tile_rows == 256)
     prefill_kernel<2><<<grid, kPreThreads, 0, stream>>>(a);

@@ -1245,6 +1245,8 @@ int prefill_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, con
   RL_TRY(check_lse(lse_out, rows, Hq));
   if (B > (1 << 22) || rows > INT32_MAX / 2 || Hq > 4096)
     return fail(RL_ERR_UNSUPPORTED, "batch, rows or head count too large");
+  // (so that places of units, at most rows / tile_tokens + 32 B, are 32-bit; more rows of heads do not fit the memory)
+  if (rows * Hq > INT32_MAX) return fail(RL_ERR_UNSUPPORTED, "rows times heads too large");
   // in-prompt offsets are formed in 32 bits
   const int64_t lim24 = (int64_t)1 << 24;
   if (k->strides[0] >= lim24 || v->strides[0] >= lim24)
@@ -1262,8 +1264,6 @@ int prefill_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, con
   a.rows_head = s.rows_head;
   a.tile_tokens = s.tile_tokens;
   a.head_blocks = s.head_blocks;
-  // (ranks of units and places of tiles are 32-bit)
-  if (rows / a.tile_tokens + 32 * B > INT32_MAX) return fail(RL_ERR_UNSUPPORTED, "rows or batch too large");
   hipStream_t st = static_cast<hipStream_t>(stream);
   Workspace* w = nullptr;
   RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
