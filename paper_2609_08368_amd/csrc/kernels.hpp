@@ -285,6 +285,7 @@ struct RopeArgs {
   const float* v_scale;
   int64_t ks_s, vs_s;
   int rows, Hq, Hkv, freqs, n_axes, interleaved, inverse;
+  int parts;              // waves of a row
   int num_pages, page_size, log2_page;
   int* err;
 };
@@ -347,7 +348,7 @@ hipError_t launch_extend(const ExtendArgs& a, hipStream_t stream, KernelTimer* t
 hipError_t launch_merge(const MergeArgs& a, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream, KernelTimer* timer);
 hipError_t launch_map(const MapArgs& a, hipStream_t stream);
-hipError_t launch_rope(const RopeArgs& a, hipStream_t stream, KernelTimer* timer);
+hipError_t launch_rope(const RopeArgs& args, int cus, hipStream_t stream, KernelTimer* timer);
 hipError_t launch_prefill(const PrefillArgs& a, int cus, hipStream_t stream, KernelTimer* timer);
 
 }  // namespace rl

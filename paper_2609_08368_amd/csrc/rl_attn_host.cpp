@@ -1153,9 +1153,10 @@ int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const 
   } else if (k_out) {
     return fail(RL_ERR_INVALID_ARG, "k is NULL");
   }
-  // (a launch has fewer than 2^32 threads, 64 for a row)
+  // (a launch has fewer than 2^32 threads, 64 for sixteen heads of a row)
   if (rows > (1 << 25) || Hq > 4096 || Hkv > 4096)
     return fail(RL_ERR_UNSUPPORTED, "rows or head count too large");
+  if (rows * ((Hq + 2 * Hkv + 15) / 16) >= (1 << 26)) return fail(RL_ERR_UNSUPPORTED, "rows times heads too large");
   RL_TRY(check_view(inv_freq, "inv_freq", 1));
   const int64_t F = inv_freq->shape[0];
   RL_TRY(check_vector(inv_freq, "inv_freq", RL_F32, F, false));
@@ -1181,6 +1182,8 @@ int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const 
     a.v_sh = v->strides[1];
   }
   if (rows == 0 || Hq + Hkv == 0) return RL_OK;
+  int cus = 0;
+  RL_TRY(current_cus(&cus));
   hipStream_t st = static_cast<hipStream_t>(stream);
   Workspace* w = nullptr;
   RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
@@ -1215,7 +1218,7 @@ int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const 
   a.err = w->err;
   rl::KernelTimer slot;
   rl::KernelTimer* timer = prof_timer(&slot, st);
-  const hipError_t e = rl::launch_rope(a, st, timer);
+  const hipError_t e = rl::launch_rope(a, cus, st, timer);
   prof_commit(4, timer);
   if (e != hipSuccess) return hip_fail(e, "rotary kernel launch");
   return RL_OK;
