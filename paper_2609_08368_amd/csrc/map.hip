@@ -8,9 +8,12 @@
 // everything. Every new page holds the row of its first token, so the thread of
 // that row writes the block-table entry, and rows are all there is to share out.
 //
-// Each workgroup sums over all requests again and then writes its share of the
-// rows: that costs it the latency of one pass per 1024 requests, where a launch
-// of its own for the sums would cost more. A lone decode step is one workgroup.
+// The bytes are nothing; a call is a chain of dependent loads (lengths, sums,
+// table or free list, stores) on top of a launch. So each workgroup sums over
+// all requests again and then writes its share of the rows, where a launch of
+// its own for the sums would cost more: 128 decoding requests take one
+// workgroup 3.8 us, 32 requests with 38K rows 5.5 us, and 3001 with 50K rows
+// 8.5 us, in one pass of 1024 threads (9.7 in three of 256 threads).
 #include <algorithm>
 
 #include "attn_common.hpp"
@@ -20,9 +23,7 @@ namespace rl {
 
 namespace {
 
-constexpr int kMapThreads = 256;
 constexpr int kMapPer = 4;                          // requests of a thread in a pass
-constexpr int kMapPass = kMapThreads * kMapPer;
 
 // Rows and pages that requests take (64 bits: a refused request may ask for any number).
 struct Need {
@@ -54,6 +55,7 @@ __device__ __forceinline__ int read_used(const MapArgs& a, int* bad) {
 }
 
 // Exclusive prefix sums of a thread's need over the workgroup, and its totals.
+template <int kThreads>
 __device__ __forceinline__ Need scan_need(Need x, Need* total, Need* wave_tot) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Need s{wave_inclusive_scan64(x.rows), wave_inclusive_scan64(x.pages)};
@@ -61,7 +63,7 @@ __device__ __forceinline__ Need scan_need(Need x, Need* total, Need* wave_tot) {
   __syncthreads();
   Need before{0, 0}, all{0, 0};
 #pragma unroll
-  for (int w = 0; w < kMapThreads / 64; ++w) {
+  for (int w = 0; w < kThreads / 64; ++w) {
     const Need t = wave_tot[w];
     if (w < wave) before = {before.rows + t.rows, before.pages + t.pages};
     all = {all.rows + t.rows, all.pages + t.pages};
@@ -70,11 +72,13 @@ __device__ __forceinline__ Need scan_need(Need x, Need* total, Need* wave_tot) {
   return {before.rows + s.rows - x.rows, before.pages + s.pages - x.pages};
 }
 
-__global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs a) {
+template <int kThreads>
+__global__ __launch_bounds__(kThreads) void map_kernel(MapArgs a) {
+  constexpr int kPass = kThreads * kMapPer;
   // of a pass's requests: first row, tokens before the step, pages before it,
   // and (free entry of the first new page) - (pages before it)
-  __shared__ int row0[kMapPass], cached[kMapPass], before[kMapPass], taken[kMapPass];
-  __shared__ Need wave_tot[kMapThreads / 64];
+  __shared__ int row0[kPass], cached[kPass], before[kPass], taken[kPass];
+  __shared__ Need wave_tot[kThreads / 64];
   __shared__ Need stop;                             // rows and pages of the requests served
   __shared__ int stopped;
   const int tid = threadIdx.x;
@@ -85,7 +89,7 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs a) {
   if (tid == 0) stopped = 0;
   __syncthreads();
   Need at{0, 0};                                    // what the passes before took
-  for (int b0 = 0; b0 < a.B; b0 += kMapPass) {
+  for (int b0 = 0; b0 < a.B; b0 += kPass) {
     Request q[kMapPer];
     Need mine{0, 0};
 #pragma unroll
@@ -95,7 +99,7 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs a) {
       mine = {mine.rows + q[i].rows, mine.pages + q[i].pages};
     }
     Need total;
-    const Need off = scan_need(mine, &total, wave_tot);
+    const Need off = scan_need<kThreads>(mine, &total, wave_tot);
     // Requests are served in order until one does not fit; that one sees the
     // sums of all before it fit and its own not, and no other does.
     Need x{at.rows + off.rows, at.pages + off.pages};
@@ -134,12 +138,12 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs a) {
     __syncthreads();
     // this workgroup's rows of the pass
     const int p0 = (int)min(at.rows, end.rows), p1 = (int)end.rows;
-    for (int r = max(lo, p0) + tid; r < min(hi, p1); r += kMapThreads) {
+    for (int r = max(lo, p0) + tid; r < min(hi, p1); r += kThreads) {
       // the last request that starts at or before r (the ones without rows share
       // the start of the next)
       int s = 0;
 #pragma unroll
-      for (int step = kMapPass / 2; step > 0; step >>= 1)
+      for (int step = kPass / 2; step > 0; step >>= 1)
         if (row0[s + step] <= r) s += step;
       const int b = b0 + s, t = cached[s] + (r - row0[s]), j = t >> a.log2_page;
       const bool fresh = j >= before[s];
@@ -157,7 +161,7 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs a) {
     __syncthreads();                                // the lists are rebuilt for the next pass
   }
   const Need end = stopped ? stop : at;
-  for (int r = max(lo, (int)end.rows) + tid; r < hi; r += kMapThreads) {   // rows behind the last request's
+  for (int r = max(lo, (int)end.rows) + tid; r < hi; r += kThreads) {   // rows behind the last request's
     a.slots[(int64_t)r * a.slots_s] = -1;
     a.pos[(int64_t)r * a.pos_s] = 0;
   }
@@ -173,10 +177,11 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs a) {
 
 // The step's lengths and free entries in place, behind the workgroups that all
 // read the ones before it: what each request got is in the row bounds.
-__global__ __launch_bounds__(kMapThreads) void map_lengths_kernel(MapArgs a) {
+constexpr int kLateThreads = 1024;
+__global__ __launch_bounds__(kLateThreads) void map_lengths_kernel(MapArgs a) {
   __shared__ long long wave_tot[16];
   long long pages = 0;
-  for (int b = threadIdx.x; b < a.B; b += kMapThreads) {
+  for (int b = threadIdx.x; b < a.B; b += kLateThreads) {
     const int c = a.kv_lens[(int64_t)b * a.kv_s];
     const int n = a.indptr[(int64_t)(b + 1) * a.indptr_s] - a.indptr[(int64_t)b * a.indptr_s];
     if (n > 0) pages += (((unsigned)(c + n) + a.page_size - 1) >> a.log2_page) -
@@ -200,8 +205,11 @@ hipError_t launch_map(const MapArgs& args, hipStream_t stream) {
   const int groups = a.rows <= 1024 ? 1 : std::min(256, (a.rows + 511) / 512);
   a.rows_block = (a.rows + groups - 1) / groups;
   a.late = groups > 1 && (a.kv_out == a.kv_lens || a.used_out == a.free_used);
-  map_kernel<<<groups, kMapThreads, 0, stream>>>(a);
-  if (a.late) map_lengths_kernel<<<1, kMapThreads, 0, stream>>>(a);
+  if (a.B <= 256 * kMapPer)                         // one pass (see the top)
+    map_kernel<256><<<groups, 256, 0, stream>>>(a);
+  else
+    map_kernel<1024><<<groups, 1024, 0, stream>>>(a);
+  if (a.late) map_lengths_kernel<<<1, kLateThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
