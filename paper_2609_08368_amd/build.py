@@ -26,11 +26,10 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build librlattn.so)")
 
 
-def build(verbose: bool = False) -> str:
-    """Compile every HIP source into librlattn.so next to this file; returns its path."""
-    out_tmp = LIB + ".tmp"
-    cmd = [
-        hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
+def compiler() -> list:
+    """hipcc with every option that decides the device code."""
+    return [
+        hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17",
         # packed FP32 instructions stay off: ordinary float code only
         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
         # device code: scores are never NaN unless the inputs are (a NaN still
@@ -38,10 +37,14 @@ def build(verbose: bool = False) -> str:
         # canonicalisation; the host code keeps full NaN semantics
         "-Xarch_device", "-fno-honor-nans",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-        "-Wall", "-Wno-unused-result",
-        *[os.path.join(CSRC, s) for s in SOURCES],
-        "-o", out_tmp,
     ]
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every HIP source into librlattn.so next to this file; returns its path."""
+    out_tmp = LIB + ".tmp"
+    cmd = [*compiler(), "-fPIC", "-shared", "-Wall", "-Wno-unused-result", *[os.path.join(CSRC, s) for s in SOURCES],
+           "-o", out_tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)

@@ -299,7 +299,7 @@ struct PrefillArgs {
   const int* indptr;      // [B + 1]
   int64_t indptr_s;
   int B, rows, Hq, Hkv, R;
-  int tile_rows;          // query rows per tile: 128 or 256
+  int tile_rows;          // query rows per tile: 64, 128 or 256
   int rows_head;          // query heads per tile
   float rows_head_inv;
   int tile_tokens;        // prompt tokens per tile

@@ -48,6 +48,26 @@ __device__ __forceinline__ void mfma_next(f32x16& c, const bf16x8& a, const bf16
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "a"(b));
 }
 
+// The last one of a chain has its result elsewhere: were it the same registers,
+// the compiler might copy the sums to the next iteration's before it, unseen. Its
+// sums stay as they are for 7 wait states more (kept).
+__device__ __forceinline__ void mfma_last(f32x16& d, const f32x16& c, const bf16x8& a, const bf16x8& b) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(d) : "v"(a), "a"(b), "v"(c));
+}
+
+// The same value, as far as the compiler knows known only from here on: what is
+// formed from it is formed here, and not kept in registers over a loop.
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ uint32_t here(uint32_t uniform) {
+  asm volatile("" : "+s"(uniform));
+  return uniform;
+}
+
+__device__ __forceinline__ void kept(const f32x16& c) { asm volatile("" ::"v"(c)); }
+
 // Rows [q0, q0 + n) of prompt b, clamped into the call's rows.
 struct Prompt {
   int q0, n;
@@ -310,14 +330,21 @@ __device__ __forceinline__ void store_block(const f32x16 (&o)[4], float inv, cha
   }
 }
 
-template <int NRB>
+// NRB blocks of 32 rows a wave; kParts = 2: the waves are two row groups times
+// two halves of a step's keys, joined at a unit's end, so that a tile has half
+// of the rows and an operand from LDS still serves as many MFMAs.
+template <int NRB, int kParts>
 __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) {
   __shared__ __attribute__((aligned(16))) char kl[kKBufs * kKSize], vl[kVBufs * kVSize];
   __shared__ __attribute__((aligned(16))) char outl[4][32 * kOutPitch];
   __shared__ Plan plan;
-  constexpr int kSlots = 32 * NRB;                 // MFMAs of a step
+  constexpr int kBlocks = 2 / kParts;              // 32-key blocks of a step for a wave
+  constexpr int kOps = 8 * kBlocks;                // operands of V, and of K, of a step
+  constexpr int kSlots = 2 * kOps * NRB;           // MFMAs of a step
+  constexpr int kGroups = 4 / kParts;              // row groups
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, kg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int part = wave / kGroups;                 // of the keys
   const int heads = a.Hkv * a.head_blocks, gh = blockIdx.x % heads;
   const int g = gh / a.head_blocks, hb = gh % a.head_blocks;
   const int w = blockIdx.x / heads, ws = gridDim.x / heads;   // workgroups of this head group
@@ -334,32 +361,43 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
   // rows of a step go from memory to LDS by the load itself: block b of 16 holds
   // rows b + 16 s (s = lane / 16), wave w fills blocks 4 w .. 4 w + 3
   const uint32_t kss = 2u * (uint32_t)a.k_st, vss = 2u * (uint32_t)a.v_st;
-  const int lrow = 16 * (lane >> 4) + 4 * wave;
-  const uint32_t lchunk = 16u * (lane & 15);
-  uint32_t kvo[4], vvo[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    kvo[i] = (uint32_t)(lrow + i) * kss + lchunk;
-    vvo[i] = (uint32_t)(lrow + i) * vss + lchunk;
-  }
-  auto load_step = [&](const char* rows, uint32_t ss, const uint32_t (&vo)[4], char* dst, int pitch, int last) {
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(dst + 4 * wave * pitch);
-    // (as assembly: see the 128-key routine in tile_attn.hpp. m0, the LDS address, is an input that the compiler sets)
+  const std::integral_constant<int, kKPitch> kpitch{};
+  const std::integral_constant<int, kVPitch> vpitch{};
+  auto load_row = [&](int t) { return 16 * ((t & 63) >> 4) + 4 * wave; };
+  auto load_chunk = [&](int t) { return 16u * (t & 15); };
+  const uint32_t kvo = (uint32_t)load_row(tid) * kss + load_chunk(tid), vvo = (uint32_t)load_row(tid) * vss + load_chunk(tid);
+  auto load_step = [&](const char* rows, uint32_t ss, uint32_t vo, char* dst, auto pitch_, int last) {
+    constexpr int kPitch = decltype(pitch_)::value;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(dst + 4 * wave * kPitch);
+    ss = here(ss);
+    uint32_t at[4];
     if (last >= kStep - 1) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(vo[i]), "s"(rows), "{m0}"(lds + i * pitch) : "memory");
+      for (int i = 0; i < 4; ++i) at[i] = vo + i * ss;
     } else {                                       // rows past the last key load that key again
+      const int t = here(tid);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"((uint32_t)min(lrow + i, last) * ss + lchunk), "s"(rows),
-                     "{m0}"(lds + i * pitch) : "memory");
+      for (int i = 0; i < 4; ++i) at[i] = (uint32_t)min(load_row(t) + i, last) * ss + load_chunk(t);
     }
+    // As assembly: see the 128-key routine in tile_attn.hpp. In one statement, since
+    // the compiler does not know it as loads: an SGPR that a vector instruction
+    // wrote (the reload of a spilled one) needs 5 wait states, and m0 needs 1.
+    asm volatile(
+        "s_mov_b32 m0, %5\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %4\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %4\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %4\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4" ::"v"(at[0]),
+        "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(rows), "s"(lds), "i"(kPitch)
+        : "memory", "m0", "scc");
   };
   auto barrier = [&]() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+  };
+  auto barrier_lds = [&]() {                       // what was written to LDS is read behind it
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
   };
   auto after = [&](int x, int size, int bufs) { return x + size == bufs * size ? 0 : x + size; };
 
@@ -385,7 +423,7 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
     int64_t row;
   };
   auto row_of = [&](const Unit& u, int thread, int rb) {
-    const int r = (thread >> 6) * (32 * NRB) + 32 * rb + (thread & 31);
+    const int r = ((thread >> 6) % kGroups) * (32 * NRB) + 32 * rb + (thread & 31);
     // r / rows_head for r < 256: r + 1/2 is at least 2^-9 of it away from a multiple
     const int ti = (int)(((float)r + 0.5f) * a.rows_head_inv), hr = r - ti * a.rows_head;
     const bool ok = ti < u.cnt && hb * a.rows_head + hr < a.R;
@@ -398,15 +436,14 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
   // what a unit needs before its first step
   auto request = [&](const Unit& u, int kb, int vb) {
     const int last = u.keys - 1;
-    load_step(u.k, kss, kvo, kl + kb, kKPitch, last);
-    if (last >= kStep) load_step(u.k + kStep * (int64_t)kss, kss, kvo, kl + after(kb, kKSize, kKBufs), kKPitch, last - kStep);
-    load_step(u.v, vss, vvo, vl + vb, kVPitch, last);
+    load_step(u.k, kss, kvo, kl + kb, kpitch, last);
+    if (last >= kStep) load_step(u.k + kStep * (int64_t)kss, kss, kvo, kl + after(kb, kKSize, kKBufs), kpitch, last - kStep);
+    load_step(u.v, vss, vvo, vl + vb, vpitch, last);
     if (last >= 2 * kStep)
-      load_step(u.k + 2 * kStep * (int64_t)kss, kss, kvo, kl + after(after(kb, kKSize, kKBufs), kKSize, kKBufs), kKPitch,
+      load_step(u.k + 2 * kStep * (int64_t)kss, kss, kvo, kl + after(after(kb, kKSize, kKBufs), kKSize, kKBufs), kpitch,
                 last - 2 * kStep);
-    if (last >= kStep) load_step(u.v + kStep * (int64_t)vss, vss, vvo, vl + after(vb, kVSize, kVBufs), kVPitch, last - kStep);
-    int t = tid;
-    asm volatile("" : "+v"(t));
+    if (last >= kStep) load_step(u.v + kStep * (int64_t)vss, vss, vvo, vl + after(vb, kVSize, kVBufs), vpitch, last - kStep);
+    const int t = here(tid);
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb) {
       const Row r = row_of(u, t, rb);
@@ -414,19 +451,19 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
     }
   };
 
-  const int kread = (col & 15) * kKPitch + (col >> 4) * 256 + 16 * kg;
+  const int kread = (col & 15) * kKPitch + (col >> 4) * 256 + 16 * kg + 512 * part;
   const int tr_row = 4 * kg + ((lane & 15) >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  const int vread = tr_row * kVPitch + 2 * tr_col;
-  // operand i of an iteration: 0 .. 15 of V (16 keys i / 4, 32 dimensions i % 4), 16 .. 31 of K (32 keys, 16 dimensions)
+  const int vread = tr_row * kVPitch + 2 * tr_col + 512 * part;
+  // operand i of an iteration: below kOps of V (16 keys i / 4, 32 dimensions i % 4), then of K (32 keys, 16 dimensions)
   auto read = [&](auto i_, const char* vb, const char* kb) -> bf16x8 {
     constexpr int i = decltype(i_)::value;
-    if constexpr (i < 16) {
+    if constexpr (i < kOps) {
       const char* vp = vb + 256 * (i >> 2) + 64 * (i & 3);
       const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)vp);
       const i16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vp + 8 * kVPitch));
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      return *reinterpret_cast<const bf16x8*>(kb + 512 * ((i - 16) >> 3) + 32 * (i & 7));
+      return *reinterpret_cast<const bf16x8*>(kb + 512 * ((i - kOps) >> 3) + 32 * (i & 7));
     }
   };
   const std::true_type yes{};
@@ -464,14 +501,14 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) {
         const Row r = row_of(u, tid, rb);
-        limit[rb] = r.ok ? u.i0 + r.ti : u.keys - 1;
+        limit[rb] = (r.ok ? u.i0 + r.ti : u.keys - 1) - 32 * part - 4 * kg;
 #pragma unroll
         for (int c = 0; c < 8; ++c) asm volatile("" : "+a"(qv[rb][c]));
       }
       barrier();                                   // the first steps' rows are in LDS
       const f32x16 zero = {};
-      f32x16 o[NRB][4], s[2][NRB];                 // O^T, and S^T(j) of the current step [32 keys][row block]
-      bf16x8 pb[NRB][4];                           // P^T(j - 1)
+      f32x16 o[NRB][4], s[kBlocks][NRB];                 // O^T, and S^T(j) of the current step [32 keys][row block]
+      bf16x8 pb[NRB][2 * kBlocks];                           // P^T(j - 1)
       bf16x8 ring[kRing];
       float nm[NRB], l[NRB], l2[NRB];              // minus the maximum, and two sums
 #pragma unroll
@@ -483,7 +520,7 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
       {
         const char* kb = kl + k0 + kread;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
             const bf16x8 x = *reinterpret_cast<const bf16x8*>(kb + 512 * b + 32 * c);
@@ -494,16 +531,17 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
         for (int rb = 0; rb < NRB; ++rb) {
           float mx = kNegInf;
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              mx = fmaxf(mx, 32 * b + 8 * (e >> 2) + 4 * kg + (e & 3) <= limit[rb] ? s[b][rb][e] : kNegInf);
-          nm[rb] = -max_l32(mx) * sl2;
+              mx = fmaxf(mx, 32 * b + 8 * (e >> 2) + (e & 3) <= limit[rb] ? s[b][rb][e] : kNegInf);
+          // (a row without a key in this part's half of the first step has none in it at all)
+          nm[rb] = kParts == 2 && limit[rb] + 4 * kg < 0 ? 0.f : -max_l32(mx) * sl2;
         }
       }
       barrier();                                   // K(0)'s buffer is free
       // buffers of V(j - 1), V(j), V(j + 2), K(j + 1), K(j + 3), and the rows that come next
-      int v_prev = 0, v_cur = v0, v_next2 = after(after(v0, kVSize, kVBufs), kVSize, kVBufs);
+      int v_cur = v0, v_next2 = after(after(v0, kVSize, kVBufs), kVSize, kVBufs), v_prev = after(v_next2, kVSize, kVBufs);
       int k_next = after(k0, kKSize, kKBufs), k_next3 = k0;
       const char* kp = u.k + 3 * kStep * (int64_t)kss;
       const char* vp = u.v + 2 * kStep * (int64_t)vss;
@@ -513,10 +551,9 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
         const char* vb = vl + v_prev + vread;
         const char* vb_next = vl + v_cur + vread;
         const char* kb = kl + k_next + kread;
-        f32x16 sn[2][NRB];
-        u32x4 pn[NRB][4];
+        f32x16 sn[kBlocks][NRB], sf[kBlocks][NRB];
+        u32x4 pn[NRB][2 * kBlocks];
         float t1, p0, p1, q0, q1;
-        const int d0 = u.keys - 1 - j * kStep - 4 * kg;
         auto finish = [&](auto x_, int part) {     // sums and conversion of pair x
           constexpr int x = decltype(x_)::value;
           if constexpr (x >= 0) {
@@ -539,7 +576,7 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
             t1 = fmaf(s[h >> 1][rb][8 * (h & 1) + e + 1], sl2, nm[rb]);
             if constexpr (kMask) {
               constexpr int z = 8 * (h & 1) + e, key = 32 * (h >> 1) + 8 * (z >> 2) + (z & 3);
-              const int d = min(limit[rb] - j * kStep - 4 * kg, d0);
+              const int d = limit[rb] - j * kStep;
               if (key > d) t0 = kNegInf;
               if (key + 1 > d) t1 = kNegInf;
             }
@@ -553,8 +590,8 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
           }
         };
         if constexpr (kS) {
-          if (j + 2 < n) load_step(vp, vss, vvo, vl + v_next2, kVPitch, u.keys - 1 - (j + 2) * kStep);
-          if (j + 3 < n) load_step(kp, kss, kvo, kl + k_next3, kKPitch, u.keys - 1 - (j + 3) * kStep);
+          if (j + 2 < n) load_step(vp, vss, vvo, vl + v_next2, vpitch, u.keys - 1 - (j + 2) * kStep);
+          if (j + 3 < n) load_step(kp, kss, kvo, kl + k_next3, kpitch, u.keys - 1 - (j + 3) * kStep);
           vp += kStep * (int64_t)vss;
           kp += kStep * (int64_t)kss;
           asm volatile("s_nop 1" ::"a"(qv[0][0]), "a"(qv[0][1]), "a"(qv[0][2]), "a"(qv[0][3]), "a"(qv[0][4]),
@@ -566,8 +603,8 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
         } else if (more) {
           request(un, k_next, after(v_cur, kVSize, kVBufs));
         }
-        constexpr int i0 = kPV ? 0 : 16, i1 = kS ? 32 : 16;
-        if constexpr (!kPV && kS) each<16, 16 + kAhead>([&](auto i) { ring[i % kRing] = read(i, vb, kb); });
+        constexpr int i0 = kPV ? 0 : kOps, i1 = kS ? 2 * kOps : kOps;
+        if constexpr (!kPV && kS) each<kOps, kOps + kAhead>([&](auto i) { ring[i % kRing] = read(i, vb, kb); });
         if constexpr (!kPV) each<0, kSlots / 2>([&](auto i) { soft(i); });
         each<i0, i1>([&](auto i) {
           // (behind the last, the first of the next iteration: values of step j)
@@ -577,16 +614,19 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
             ring[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead - i1>{}, vb_next, kb);
           __builtin_amdgcn_sched_barrier(0);
           each<0, NRB>([&](auto rb) {
-            if constexpr (i < 16)
+            if constexpr (i < kOps)
               o[rb][i & 3] = mfma_32x32x16(ring[i % kRing], pb[rb][i >> 2], o[rb][i & 3]);
             else if constexpr ((i & 7) == 0)
-              mfma_first(sn[(i - 16) >> 3][rb], ring[i % kRing], qv[rb][0]);
+              mfma_first(sn[(i - kOps) >> 3][rb], ring[i % kRing], qv[rb][0]);
+            else if constexpr ((i & 7) == 7)
+              mfma_last(sf[(i - kOps) >> 3][rb], sn[(i - kOps) >> 3][rb], ring[i % kRing], qv[rb][7]);
             else
-              mfma_next(sn[(i - 16) >> 3][rb], ring[i % kRing], qv[rb][i & 7]);
+              mfma_next(sn[(i - kOps) >> 3][rb], ring[i % kRing], qv[rb][i & 7]);
             __builtin_amdgcn_sched_barrier(0);
             soft(std::integral_constant<int, NRB * i + rb>{});
             __builtin_amdgcn_sched_barrier(0);
           });
+          if constexpr (kBlocks == 2 && i == kOps + 8) each<0, NRB>([&](auto rb) { kept(sn[0][rb]); });
         });
         if constexpr (!kS) each<kSlots / 2, kSlots>([&](auto i) { soft(i); });
         q0 = p0;
@@ -596,17 +636,20 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) asm volatile("" : "+v"(l[rb]), "+v"(l2[rb]));
         if constexpr (i0 == i1) each<0, kAhead>([&](auto i) { ring[i] = read(i, vb_next, kb); });
-        if constexpr (kS) asm volatile("s_nop 11" ::: "memory");   // S^T(j + 1) is complete
+        if constexpr (kS) {
+          asm volatile("s_nop 11" ::: "memory");   // S^T(j + 1) is complete
+          each<0, NRB>([&](auto rb) { kept(sn[kBlocks - 1][rb]); });
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
-          for (int h = 0; h < 4; ++h) pb[rb][h] = __builtin_bit_cast(bf16x8, pn[rb][h]);
+          for (int h = 0; h < 2 * kBlocks; ++h) pb[rb][h] = __builtin_bit_cast(bf16x8, pn[rb][h]);
         if constexpr (kS) {
 #pragma unroll
-          for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int rb = 0; rb < NRB; ++rb) s[b][rb] = sn[b][rb];
+            for (int rb = 0; rb < NRB; ++rb) s[b][rb] = sf[b][rb];
         }
       };
       auto turn = [&](int j) {
@@ -644,8 +687,8 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
       // the values of the last step (its first operands are read)
       {
         const char* vb = vl + v_cur + vread;
-        each<0, 16>([&](auto i) {
-          if constexpr (i + kAhead < 16)
+        each<0, kOps>([&](auto i) {
+          if constexpr (i + kAhead < kOps)
             ring[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead>{}, vb, vb);
 #pragma unroll
           for (int rb = 0; rb < NRB; ++rb)
@@ -656,16 +699,50 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
       v0 = after(v_cur, kVSize, kVBufs);
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) l[rb] += l2[rb];
-      // (formed again: kept over the loop they would cost registers)
-      int t = tid;
-      asm volatile("" : "+v"(t));
+      if constexpr (kParts == 2) {
+        // The second parts' sums join the first's, 16 KB of a row block at a time
+        // through the V buffers that hold nothing any more (of the last two steps).
+        float* const buf = reinterpret_cast<float*>(vl + (wave % kGroups ? v_cur : v_prev)) + 4 * lane;
+        float* const ml = reinterpret_cast<float*>(outl[2 + wave % kGroups]) + 2 * lane;
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+          barrier_lds();
+          if (part == 1) {
+            ml[0] = sum_l32(l[rb]);
+            ml[1] = -nm[rb];
+#pragma unroll
+            for (int jd = 0; jd < 4; ++jd)
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4*>(buf + 256 * (4 * jd + q)) =
+                    f32x4{o[rb][jd][4 * q], o[rb][jd][4 * q + 1], o[rb][jd][4 * q + 2], o[rb][jd][4 * q + 3]};
+          }
+          barrier_lds();
+          if (part == 0) {
+            const float l1 = ml[0], m0 = -nm[rb], m1 = l1 == 0.f ? kNegInf : ml[1], m = fmaxf(m0, m1);
+            const float w0 = exp2_fast(m0 - m), w1 = exp2_fast(m1 - m);
+            l[rb] = l[rb] * w0 + (kg ? 0.f : l1 * w1);
+            nm[rb] = -m;
+#pragma unroll
+            for (int jd = 0; jd < 4; ++jd)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(buf + 256 * (4 * jd + q));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[rb][jd][4 * q + i] = fmaf(x[i], w1, o[rb][jd][4 * q + i] * w0);
+              }
+          }
+        }
+      }
+      const int t = here(tid);
+      const bool mine = kParts == 1 || part == 0;  // these rows are this wave's to store
       const bool again = __builtin_amdgcn_ballot_w64(odd_values<NRB>(o, l)) != 0;
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the next unit's rows have come (before the stores, which need not)
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) {
         const float l_tot = sum_l32(l[rb]);
         const Row r = row_of(u, t, rb);
-        if (again) continue;
+        if (again || !mine) continue;
         const float inv = 1.f / l_tot;
         auto row = [&](auto* out, int i, bool* ok) {
           const Row x = row_of(u, (t & ~63) + i, rb);
@@ -679,9 +756,9 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
         if (a.lse && r.ok && (t & 63) < 32)
           a.lse[r.row * a.lse_st + (int64_t)r.head * a.lse_sh] = (__builtin_amdgcn_logf(l_tot) - nm[rb]) * kLn2;
       }
-      if (again) {
+      if (again && mine) {
         for (int rb = 0; rb < NRB; ++rb)
-          attend_again((ConstPrefillArgs*)__builtin_amdgcn_kernarg_segment_ptr(), wave * (32 * NRB) + 32 * rb, u.q0, u.i0,
+          attend_again((ConstPrefillArgs*)__builtin_amdgcn_kernarg_segment_ptr(), wave % kGroups * (32 * NRB) + 32 * rb, u.q0, u.i0,
                        u.cnt, g, hb);
       }
       if (!more) break;
@@ -704,9 +781,11 @@ hipError_t launch_prefill(const PrefillArgs& args, int cus, hipStream_t stream, 
   a.rows_head_inv = 1.f / (float)a.rows_head;
   if (timer) (void)hipEventRecord(timer->start, stream);
   if (a.tile_rows == 256)
-    prefill_kernel<2><<<grid, kPreThreads, 0, stream>>>(a);
+    prefill_kernel<2, 1><<<grid, kPreThreads, 0, stream>>>(a);
+  else if (a.tile_rows == 128)
+    prefill_kernel<2, 2><<<grid, kPreThreads, 0, stream>>>(a);
   else
-    prefill_kernel<1><<<grid, kPreThreads, 0, stream>>>(a);
+    prefill_kernel<1, 2><<<grid, kPreThreads, 0, stream>>>(a);
   if (timer) (void)hipEventRecord(timer->stop, stream);
   return hipGetLastError();
 }

@@ -1034,6 +1034,12 @@ int map_impl(const rl_tensor* kv_lens, const rl_tensor* new_lens, const rl_tenso
     return fail(RL_ERR_UNSUPPORTED, "block_table: strides must be positive, the column stride below 2^24");
   RL_TRY(check_data(block_table, "block_table"));
   RL_TRY(check_vector(kv_lens_out, "kv_lens_out", RL_I32, B, true));
+  // kv_lens itself, or memory of its own (columns of one buffer lie in one range, but do not meet)
+  const int64_t apart = static_cast<const int*>(kv_lens_out->data) - static_cast<const int*>(kv_lens->data);
+  const int64_t s_in = kv_lens->strides[0], s_out = kv_lens_out->strides[0];
+  if (B > 1 && (s_in != s_out || (apart != 0 && apart % s_out == 0)) && apart <= (B - 1) * s_in &&
+      -apart <= (B - 1) * s_out)
+    return fail(RL_ERR_UNSUPPORTED, "kv_lens_out must be kv_lens or not overlap it");
   RL_TRY(check_vector(free_used_out, "free_used_out", RL_I32, 1, true));
   RL_TRY(check_vector(qo_indptr, "qo_indptr", RL_I32, B + 1, true));
   RL_TRY(check_view(slot_map, "slot_map", 1));
@@ -1087,7 +1093,10 @@ int check_head_rows(const rl_tensor* t, const char* name, int64_t rows, int64_t 
   RL_TRY(check_rows128(t, name));
   if (t->shape[0] != rows || t->shape[1] != heads)
     return fail(RL_ERR_SHAPE, "%s must be [%lld, %lld, 128]", name, (long long)rows, (long long)heads);
-  if (written && ((rows > 1 && t->strides[0] < 128) || (heads > 1 && t->strides[1] < 128)))
+  // one of the two strides steps over all that the other one reaches
+  const int64_t s0 = t->strides[0], s1 = t->strides[1];
+  if (written && ((rows > 1 && s0 < 128) || (heads > 1 && s1 < 128) ||
+                  (rows > 1 && heads > 1 && s0 < (heads - 1) * s1 + 128 && s1 < (rows - 1) * s0 + 128)))
     return fail(RL_ERR_UNSUPPORTED, "%s: rows that are written must not overlap", name);
   return check_data(t, name);
 }
@@ -1259,10 +1268,15 @@ int prefill_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, con
   rl::PrefillArgs a{};
   int cus = 0;
   RL_TRY(current_cus(&cus));
-  // tiles of 128 rows where those of 256 would leave CUs idle (see the kernel)
+  // The largest tile that gives every CU a unit, as far as the sizes tell (half a tile more a prompt). One prompt of
+  // 4095 rows of 8 + 2 heads took 97 us in tiles of 256, 68 of 128 and 59 of 64; of 8192 rows 190, 152 and 194; of
+  // 4095 rows of 32 + 8 heads 135, 162 and 201; four of 300 rows of 64 + 8 heads 30, 38 and 36.
   const int64_t R = Hq / Hkv;
-  auto units = [&](const ExtendShape& x) { return (rows / x.tile_tokens + B) * Hkv * x.head_blocks; };
-  a.tile_rows = units(extend_shape(R)) < cus ? 128 : 256;
+  auto few = [&](int tile_rows) {
+    const ExtendShape x = extend_shape(R, tile_rows);
+    return (rows / x.tile_tokens + B / 2) * Hkv * x.head_blocks <= cus;
+  };
+  a.tile_rows = !few(256) ? 256 : !few(128) ? 128 : 64;
   const ExtendShape s = extend_shape(R, a.tile_rows);
   a.rows_head = s.rows_head;
   a.tile_tokens = s.tile_tokens;

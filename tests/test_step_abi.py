@@ -58,6 +58,9 @@ def map_args(B=3, T=10, **kw):
     (dict(table=fake([3, 4], I32, strides=[0, 1])), "RL_ERR_UNSUPPORTED", "block_table"),
     (dict(table=fake([3, 4], I32, strides=[4, 0])), "RL_ERR_UNSUPPORTED", "block_table"),
     (dict(kv_out=fake([3], I32, strides=[0])), "RL_ERR_UNSUPPORTED", "kv_lens_out: stride"),
+    (dict(kv_out=fake([3], I32, strides=[2])), "RL_ERR_UNSUPPORTED", "kv_lens_out must be kv_lens or not overlap it"),
+    (dict(kv_out=fake([3], I32, ptr=FAKE + 4)), "RL_ERR_UNSUPPORTED", "kv_lens_out must be kv_lens or not overlap it"),
+    (dict(kv_out=fake([3], I32, ptr=FAKE - 8)), "RL_ERR_UNSUPPORTED", "kv_lens_out must be kv_lens or not overlap it"),
     (dict(ptr=fake([3], I32)), "RL_ERR_SHAPE", "qo_indptr must have 4"),
     (dict(slots=fake([10], I32)), "RL_ERR_DTYPE", "slot_map must be int64"),
     (dict(slots=fake([1 << 31], I64)), "RL_ERR_UNSUPPORTED", "too long"),
@@ -66,6 +69,15 @@ def map_args(B=3, T=10, **kw):
 ])
 def test_map_slots_refuses(change, status, needle):
     refused(ra.lib().rl_attn_map_slots, map_args(**change), status, needle)
+
+
+@pytest.mark.parametrize("change", [
+    dict(kv_out=fake([3], I32, ptr=FAKE + 12)), dict(kv_out=fake([3], I32, ptr=FAKE - 12)),
+    dict(kv=fake([3], I32, strides=[2]), kv_out=fake([3], I32, strides=[2], ptr=FAKE + 4)),
+    dict(kv=fake([3], I32, strides=[2]), kv_out=fake([3], I32, strides=[2]))])
+def test_map_slots_takes_lengths_beside_each_other(change):
+    """(as far as the check of its last argument)"""
+    refused(ra.lib().rl_attn_map_slots, map_args(**change, pos=fake([9], I32)), "RL_ERR_SHAPE", "positions must have 10")
 
 
 def rope_args(T=10, hq=8, hkv=2, F=64, **kw):
@@ -82,6 +94,8 @@ ROPE_REFUSALS = [
     (dict(q_out=None), "RL_ERR_INVALID_ARG", "q_out is NULL"),
     (dict(q_out=fake([10, 7, 128], BF16)), "RL_ERR_SHAPE", "q_out must be [10, 8, 128]"),
     (dict(q_out=fake([10, 8, 128], BF16, strides=[1024, 0, 1])), "RL_ERR_UNSUPPORTED", "must not overlap"),
+    (dict(q_out=fake([10, 8, 128], BF16, strides=[256, 128, 1])), "RL_ERR_UNSUPPORTED", "must not overlap"),
+    (dict(q_out=fake([10, 8, 128], BF16, strides=[128, 1272, 1])), "RL_ERR_UNSUPPORTED", "must not overlap"),
     (dict(k_out=fake([9, 2, 128], BF16)), "RL_ERR_SHAPE", "k_out"),
     (dict(pos=fake([10], I32)), "RL_ERR_SHAPE", "positions must have 2"),
     (dict(pos=fake([3, 9], I32)), "RL_ERR_SHAPE", "positions must be"),
