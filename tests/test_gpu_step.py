@@ -467,6 +467,45 @@ def test_prefill_of_extreme_scores():
         assert np.all(np.abs(H.f64(lse) - ref[1]) <= 1e-4 * np.maximum(1, np.abs(ref[1])))
 
 
+# (prompts whose tiles have 64, 128 and 256 rows on a device of 256 CUs, and their neighbours in length)
+@pytest.mark.parametrize("case", [
+    ([511], 32, 8), ([513], 32, 8), ([2000], 32, 8), ([1500, 0, 500], 32, 8), ([2111], 32, 8), ([63, 65], 96, 96),
+    ([129, 127], 64, 64), ([800], 128, 128), ([33, 1, 31], 5, 1), ([600], 128, 1), ([300, 40], 70, 1)], ids=str)
+def test_prefill_of_every_tile(case):
+    lens, hq, hkv = case
+    c = prompts(sum(lens) + hq, lens, hq, hkv, pad=2)
+    ref = step.prefill(bits(c["q"]), bits(c["k"]), bits(c["v"]), c["indptr"], 128 ** -0.5)
+    rows = int(c["indptr"][-1])
+    for dtype in (torch.bfloat16, torch.float32):
+        out, lse = run_prefill(c, dtype)
+        check_rows(out[:rows], lse[:rows], ref[0][:rows], ref[1][:rows], ref[2][:rows], f32=dtype == torch.float32,
+                   what=f"{case}")
+        assert torch.isnan(out[rows:].float()).all() and torch.isnan(lse[rows:]).all(), "rows behind the last prompt"
+        again, _ = run_prefill(c, dtype)
+        assert torch.equal(out[:rows], again[:rows]), "repeatable"
+
+
+@pytest.mark.parametrize("hq,hkv", [(96, 96), (128, 64)])
+def test_prefill_of_large_tiles_sees_nothing_behind_a_row(hq, hkv):
+    test_prefill_sees_nothing_behind_a_row(hq, hkv)
+
+
+@pytest.mark.parametrize("lens,hq,hkv", [([511], 32, 8), ([2000], 32, 8), ([800], 128, 128)], ids=str)
+def test_prefill_of_scores_that_outgrow_the_first_keys(lens, hq, hkv):
+    """A row's largest score comes late and lies hundreds above (or all lie far below) those of its first keys."""
+    c = prompts(41, lens, hq, hkv)
+    d = dict(c, q=c["q"].abs(), k=c["k"].abs().float())
+    ramp = torch.linspace(-1.0, 1.0, lens[0], device=DEV)[:, None, None]
+    for late in (ramp, -ramp, ramp.abs() - 0.5, torch.where(ramp > 0.5, 60.0, -60.0)):
+        d["k"] = (c["k"].abs().float() * 40 * late).to(torch.bfloat16)
+        ref = step.prefill(bits(d["q"]), bits(d["k"]), bits(d["v"]), d["indptr"], 128 ** -0.5)
+        out, lse = run_prefill(d)
+        mag = np.abs(H.f64(d["q"])).sum(-1).max() * np.abs(H.f64(d["k"])).max() * 128 ** -0.5
+        tol = (2.0 ** -8 + 2 * 128 * 2.0 ** -24 * mag) * ref[2] + 2.0 ** -8 * np.abs(ref[0])
+        assert np.all(np.abs(H.f64(out) - ref[0]) <= tol)
+        assert np.all(np.abs(H.f64(lse) - ref[1]) <= 1e-4 * np.maximum(1, np.abs(ref[1])))
+
+
 def test_prefill_reads_strides():
     c = prompts(41, [100, 37], 8, 2)
     want, want_lse = run_prefill(c)
