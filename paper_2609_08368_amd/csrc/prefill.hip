@@ -303,10 +303,10 @@ __device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int
 // instruction writes whole lines of eight rows. row(i, ok): address of row i.
 constexpr int kOutPitch = 128 + 16;
 template <typename T, typename RowOf>
-__device__ __forceinline__ void store_block(const f32x16 (&o)[4], float inv, char* lds, RowOf&& row) {
+__device__ __forceinline__ void store_block(const f32x16 (&o)[4], float inv, char* lds, int lane, RowOf&& row) {
   constexpr int kJd = 4 / sizeof(T);               // 32-dimension blocks in 128 bytes
   typedef T t4 __attribute__((ext_vector_type(4)));
-  const int lane = threadIdx.x & 63, col = lane & 31, kg = lane >> 5;
+  const int col = lane & 31, kg = lane >> 5;
   T* to[4];
   bool ok[4];
 #pragma unroll
@@ -750,9 +750,9 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
           return out + x.row * a.out_st + (int64_t)x.head * a.out_sh;
         };
         if (a.out_f32)
-          store_block<float>(o[rb], inv, outl[wave], [&](int i, bool* ok) { return row((float*)a.out, i, ok); });
+          store_block<float>(o[rb], inv, outl[wave], t & 63, [&](int i, bool* ok) { return row((float*)a.out, i, ok); });
         else
-          store_block<__bf16>(o[rb], inv, outl[wave], [&](int i, bool* ok) { return row((__bf16*)a.out, i, ok); });
+          store_block<__bf16>(o[rb], inv, outl[wave], t & 63, [&](int i, bool* ok) { return row((__bf16*)a.out, i, ok); });
         if (a.lse && r.ok && (t & 63) < 32)
           a.lse[r.row * a.lse_st + (int64_t)r.head * a.lse_sh] = (__builtin_amdgcn_logf(l_tot) - nm[rb]) * kLn2;
       }
