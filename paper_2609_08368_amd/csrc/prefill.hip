@@ -429,25 +429,34 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
     const bool ok = ti < u.cnt && hb * a.rows_head + hr < a.R;
     return Row{ok, ti, g * a.R + hb * a.rows_head + (ok ? hr : 0), (int64_t)(u.q0 + u.i0 + (ok ? ti : 0))};
   };
-  auto q_at = [&](const Row& r) { return (const __bf16*)a.q + r.row * a.q_st + (int64_t)r.head * a.q_sh; };
 
   bf16x8 qv[NRB][8];
   int k0 = 0, v0 = 0;                              // buffers of a unit's first step
-  // what a unit needs before its first step
-  auto request = [&](const Unit& u, int kb, int vb) {
+  // What a unit needs before its first step, in kPieces loads: rows of K and V
+  // steps (a step is one piece), then the query rows, 16 dimensions a piece.
+  constexpr int kPieces = 5 + 8 * NRB;
+  auto request = [&](auto piece, const __bf16*& q_row, const Unit& u, int kb, int vb) {
+    constexpr int p = decltype(piece)::value;
     const int last = u.keys - 1;
-    load_step(u.k, kss, kvo, kl + kb, kpitch, last);
-    if (last >= kStep) load_step(u.k + kStep * (int64_t)kss, kss, kvo, kl + after(kb, kKSize, kKBufs), kpitch, last - kStep);
-    load_step(u.v, vss, vvo, vl + vb, vpitch, last);
-    if (last >= 2 * kStep)
-      load_step(u.k + 2 * kStep * (int64_t)kss, kss, kvo, kl + after(after(kb, kKSize, kKBufs), kKSize, kKBufs), kpitch,
-                last - 2 * kStep);
-    if (last >= kStep) load_step(u.v + kStep * (int64_t)vss, vss, vvo, vl + after(vb, kVSize, kVBufs), vpitch, last - kStep);
-    const int t = here(tid);
-#pragma unroll
-    for (int rb = 0; rb < NRB; ++rb) {
-      const Row r = row_of(u, t, rb);
-      load_q_operand(q_at(r), r.ok, qv[rb]);
+    if constexpr (p < 5) {
+      constexpr int step = p < 2 ? p : p == 3 ? 2 : p / 4;   // K(0), K(1), V(0), K(2), V(1)
+      if (last < step * kStep) return;
+      if constexpr (p == 2 || p == 4)
+        load_step(u.v + step * kStep * (int64_t)vss, vss, vvo, vl + (step ? after(vb, kVSize, kVBufs) : vb), vpitch,
+                  last - step * kStep);
+      else
+        load_step(u.k + step * kStep * (int64_t)kss, kss, kvo,
+                  kl + (step == 0   ? kb
+                        : step == 1 ? after(kb, kKSize, kKBufs)
+                                    : after(after(kb, kKSize, kKBufs), kKSize, kKBufs)),
+                  kpitch, last - step * kStep);
+    } else {
+      constexpr int rb = (p - 5) / 8, c = (p - 5) % 8;
+      if constexpr (c == 0) {
+        const Row r = row_of(u, here(tid), rb);
+        q_row = (const __bf16*)a.q + r.row * a.q_st + (int64_t)r.head * a.q_sh + 8 * kg;
+      }
+      qv[rb][c] = load_bf16x8(q_row + 16 * c);     // (a row past the tile's is its first one again, and not stored)
     }
   };
 
@@ -486,7 +495,8 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
     if (at < kPreThreads && __builtin_amdgcn_readfirstlane(plan.units[at].w) == kEnd) break;
     if (at == kPreThreads) continue;
     Unit u = unit_at(at);
-    request(u, k0, v0);
+    const __bf16* q_first;
+    each<0, kPieces>([&](auto p) { request(p, q_first, u, k0, v0); });
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     bool end = false;
     for (;;) {
@@ -530,13 +540,14 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
 #pragma unroll
         for (int rb = 0; rb < NRB; ++rb) {
           float mx = kNegInf;
+          const int lim = here(limit[rb]);         // (else the compiler keeps these comparisons for the softmax)
 #pragma unroll
           for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              mx = fmaxf(mx, 32 * b + 8 * (e >> 2) + (e & 3) <= limit[rb] ? s[b][rb][e] : kNegInf);
+              mx = fmaxf(mx, 32 * b + 8 * (e >> 2) + (e & 3) <= lim ? s[b][rb][e] : kNegInf);
           // (a row without a key in this part's half of the first step has none in it at all)
-          nm[rb] = kParts == 2 && limit[rb] + 4 * kg < 0 ? 0.f : -max_l32(mx) * sl2;
+          nm[rb] = kParts == 2 && lim + 4 * kg < 0 ? 0.f : -max_l32(mx) * sl2;
         }
       }
       barrier();                                   // K(0)'s buffer is free
@@ -600,12 +611,21 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
             asm volatile("s_nop 1" ::"a"(qv[NRB - 1][0]), "a"(qv[NRB - 1][1]), "a"(qv[NRB - 1][2]), "a"(qv[NRB - 1][3]),
                          "a"(qv[NRB - 1][4]), "a"(qv[NRB - 1][5]), "a"(qv[NRB - 1][6]), "a"(qv[NRB - 1][7]));
           __builtin_amdgcn_sched_barrier(0);
-        } else if (more) {
-          request(un, k_next, after(v_cur, kVSize, kVBufs));
         }
+        // the next unit's loads between the products and the exponentials of this one's last step
+        constexpr int kReq = kPV ? kSlots / 2 : kSlots;
+        const __bf16* q_next;
+        auto spread = [&](auto slot_) {
+          constexpr int slot = decltype(slot_)::value;
+          if constexpr (!kS && slot < kReq) {
+            if (more)
+              each<slot * kPieces / kReq, (slot + 1) * kPieces / kReq>(
+                  [&](auto p) { request(p, q_next, un, k_next, after(v_cur, kVSize, kVBufs)); });
+          }
+        };
         constexpr int i0 = kPV ? 0 : kOps, i1 = kS ? 2 * kOps : kOps;
         if constexpr (!kPV && kS) each<kOps, kOps + kAhead>([&](auto i) { ring[i % kRing] = read(i, vb, kb); });
-        if constexpr (!kPV) each<0, kSlots / 2>([&](auto i) { soft(i); });
+        if constexpr (!kPV) each<0, kSlots / 2>([&](auto i) { spread(i); soft(i); });
         each<i0, i1>([&](auto i) {
           // (behind the last, the first of the next iteration: values of step j)
           if constexpr (i + kAhead < i1)
@@ -624,11 +644,12 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
               mfma_next(sn[(i - kOps) >> 3][rb], ring[i % kRing], qv[rb][i & 7]);
             __builtin_amdgcn_sched_barrier(0);
             soft(std::integral_constant<int, NRB * i + rb>{});
+            spread(std::integral_constant<int, NRB * i + rb>{});
             __builtin_amdgcn_sched_barrier(0);
           });
           if constexpr (kBlocks == 2 && i == kOps + 8) each<0, NRB>([&](auto rb) { kept(sn[0][rb]); });
         });
-        if constexpr (!kS) each<kSlots / 2, kSlots>([&](auto i) { soft(i); });
+        if constexpr (!kS) each<kSlots / 2, kSlots>([&](auto i) { spread(i); soft(i); });
         q0 = p0;
         q1 = p1;
         finish(std::integral_constant<int, kSlots / 2 - 1>{}, 0);
