@@ -3,7 +3,36 @@
 //
 // A unit of work is (prompt b, KV head g, block of query heads, run of tokens):
 // up to 256 query rows, token-major (row r -> token r / RB, head r % RB), which
-// all read the same keys.
+// all read the same keys in steps of 64.
+//
+// S^T = K Q^T and O^T += V^T P^T on 32x32x16 MFMAs, so that a row is a column:
+// its scores, maximum and sums are in two lanes, and P^T is an operand of the
+// second product as it comes. Four waves, one a SIMD with all 512 registers, of
+// 64 rows each: an operand read from LDS serves two MFMAs (with 32 rows, and
+// eight waves, a 16K prompt of 64 + 8 heads took 4.4 ms against 3.6, bound by
+// those reads). A wave's step is one stream: values of step j - 1, softmax of
+// step j and scores of step j + 1, in which each MFMA is followed by the four or
+// five vector instructions of a softmax slot, which run beside it. Rows of K and
+// V go from memory to LDS by the load, two and three steps ahead, one barrier a
+// step.
+//
+// There is no running maximum: a row's probabilities are taken against the
+// maximum of its first keys, which in 32-bit floats is as good unless a later
+// score is 88 above it. Then a sum or O is infinite or NaN at the end, as it is
+// where a masked value is (0 times infinity), and the wave computes its rows
+// again, slowly and with a running maximum (attend_again). The running maximum
+// costs 7% of a 16K prompt.
+//
+// Workgroups stay, one a CU, and take units from a longest-first order that each
+// of them works out alike (plan_levels); a unit's first rows are requested in
+// the last step of the one before.
+//
+// MFMA-bound: a 16384-row prompt of 64 + 8 heads runs at 1.20-1.25 PFLOP/s
+// (3.5-3.7 ms, box to box; a large bf16 matrix product of the library runs at
+// 1.22), a step of 256 rows in 3200 cycles where its MFMAs alone take 2048. Short
+// prompts pay a unit's 9,000 cycles around its steps (operands and scores of the
+// first one, the last values, rows out): 24 prompts of up to 701 rows of 96 + 8
+// heads run at 0.47 PFLOP/s (221 us, 2.1 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -297,10 +326,9 @@ __device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int
 }
 
 // A wave's 32 rows to memory. O^T has a row's dimensions in two lanes, four
-// neighbours at a time, so stores from there would touch 32 rows each with 16
-// bytes (which took 9,000 cycles a unit: an instruction costs a cycle or two per
-// line); through LDS (wave-private, 128 bytes of each row at once) an
-// instruction writes whole lines of eight rows. row(i, ok): address of row i.
+// neighbours at a time; through LDS (wave-private, 128 bytes of each row at once)
+// a store instruction writes whole lines of eight rows instead of 16 bytes of 32.
+// row(i, ok): address of row i.
 constexpr int kOutPitch = 128 + 16;
 template <typename T, typename RowOf>
 __device__ __forceinline__ void store_block(const f32x16 (&o)[4], float inv, char* lds, int lane, RowOf&& row) {
@@ -338,6 +366,7 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
   __shared__ __attribute__((aligned(16))) char kl[kKBufs * kKSize], vl[kVBufs * kVSize];
   __shared__ __attribute__((aligned(16))) char outl[4][32 * kOutPitch];
   __shared__ Plan plan;
+  __shared__ int64_t q_off[kPreThreads], out_off[kPreThreads];   // elements from a tile's first row of its first head
   constexpr int kBlocks = 2 / kParts;              // 32-key blocks of a step for a wave
   constexpr int kOps = 8 * kBlocks;                // operands of V, and of K, of a step
   constexpr int kSlots = 2 * kOps * NRB;           // MFMAs of a step
@@ -349,6 +378,14 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
   const int g = gh / a.head_blocks, hb = gh % a.head_blocks;
   const int w = blockIdx.x / heads, ws = gridDim.x / heads;   // workgroups of this head group
   const float sl2 = a.scale * kLog2e;
+  const int row0 = wave % kGroups * (32 * NRB);    // of the wave in the tile
+  const int64_t head0 = g * a.R + hb * a.rows_head;
+  {
+    const int ti = tid / a.rows_head, hr = tid - ti * a.rows_head;
+    const bool head_ok = hb * a.rows_head + hr < a.R;
+    q_off[tid] = head_ok ? ti * a.q_st + hr * a.q_sh : 0;
+    out_off[tid] = head_ok ? ti * a.out_st + hr * a.out_sh : -1;
+  }
   int bad = 0;
   if (a.B <= kSorted) {
     plan_levels(a, plan, &bad);
@@ -432,31 +469,27 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
 
   bf16x8 qv[NRB][8];
   int k0 = 0, v0 = 0;                              // buffers of a unit's first step
-  // What a unit needs before its first step, in kPieces loads: rows of K and V
-  // steps (a step is one piece), then the query rows, 16 dimensions a piece.
-  constexpr int kPieces = 5 + 8 * NRB;
-  auto request = [&](auto piece, const __bf16*& q_row, const Unit& u, int kb, int vb) {
-    constexpr int p = decltype(piece)::value;
+  // what a unit needs before its first step; its query rows as they lie in memory, 16 lanes a row
+  auto request = [&](const Unit& u, int kb, int vb) {
     const int last = u.keys - 1;
-    if constexpr (p < 5) {
-      constexpr int step = p < 2 ? p : p == 3 ? 2 : p / 4;   // K(0), K(1), V(0), K(2), V(1)
-      if (last < step * kStep) return;
-      if constexpr (p == 2 || p == 4)
-        load_step(u.v + step * kStep * (int64_t)vss, vss, vvo, vl + (step ? after(vb, kVSize, kVBufs) : vb), vpitch,
-                  last - step * kStep);
-      else
-        load_step(u.k + step * kStep * (int64_t)kss, kss, kvo,
-                  kl + (step == 0   ? kb
-                        : step == 1 ? after(kb, kKSize, kKBufs)
-                                    : after(after(kb, kKSize, kKBufs), kKSize, kKBufs)),
-                  kpitch, last - step * kStep);
-    } else {
-      constexpr int rb = (p - 5) / 8, c = (p - 5) % 8;
-      if constexpr (c == 0) {
-        const Row r = row_of(u, here(tid), rb);
-        q_row = (const __bf16*)a.q + r.row * a.q_st + (int64_t)r.head * a.q_sh + 8 * kg;
-      }
-      qv[rb][c] = load_bf16x8(q_row + 16 * c);     // (a row past the tile's is its first one again, and not stored)
+    load_step(u.k, kss, kvo, kl + kb, kpitch, last);
+    if (last >= kStep) load_step(u.k + kStep * (int64_t)kss, kss, kvo, kl + after(kb, kKSize, kKBufs), kpitch, last - kStep);
+    load_step(u.v, vss, vvo, vl + vb, vpitch, last);
+    if (last >= 2 * kStep)
+      load_step(u.k + 2 * kStep * (int64_t)kss, kss, kvo, kl + after(after(kb, kKSize, kKBufs), kKSize, kKBufs), kpitch,
+                last - 2 * kStep);
+    if (last >= kStep) load_step(u.v + kStep * (int64_t)vss, vss, vvo, vl + after(vb, kVSize, kVBufs), vpitch, last - kStep);
+    const int t = here(tid), rows = u.cnt * a.rows_head;
+    const __bf16* qb = (const __bf16*)a.q + (int64_t)(u.q0 + u.i0) * a.q_st + head0 * a.q_sh + 8 * (t & 15);
+    const int r0 = row0 + ((t & 63) >> 4);
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb) {
+      int64_t off[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) off[i] = q_off[r0 + 32 * rb + 4 * i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)                  // (a row past the tile's is its first one again, and not stored)
+        qv[rb][i] = load_bf16x8(qb + (r0 + 32 * rb + 4 * i < rows ? off[i] : 0));
     }
   };
 
@@ -495,8 +528,7 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
     if (at < kPreThreads && __builtin_amdgcn_readfirstlane(plan.units[at].w) == kEnd) break;
     if (at == kPreThreads) continue;
     Unit u = unit_at(at);
-    const __bf16* q_first;
-    each<0, kPieces>([&](auto p) { request(p, q_first, u, k0, v0); });
+    request(u, k0, v0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     bool end = false;
     for (;;) {
@@ -512,10 +544,30 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
       for (int rb = 0; rb < NRB; ++rb) {
         const Row r = row_of(u, tid, rb);
         limit[rb] = (r.ok ? u.i0 + r.ti : u.keys - 1) - 32 * part - 4 * kg;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) asm volatile("" : "+a"(qv[rb][c]));
       }
       barrier();                                   // the first steps' rows are in LDS
+      int v_cur = v0, v_next2 = after(after(v0, kVSize, kVBufs), kVSize, kVBufs), v_prev = after(v_next2, kVSize, kVBufs);
+      {
+        // The query rows become MFMA operands through the V buffers that nothing is in, half of one a wave. (Loaded as
+        // operands, 32 rows with 16 bytes of each lane, they kept the load path busy for 4 times as long.)
+        constexpr int kPitch = 256 + 16;
+        static_assert(64 * kPitch == kVSize, "two waves' rows in a buffer");
+        const int t = here(tid) & 63;
+        char* const own = vl + (wave & 2 ? v_prev : v_next2) + (wave & 1) * (32 * kPitch);
+        char* const to = own + (t >> 4) * kPitch + 16 * (t & 15);
+        const char* const from = own + (t & 31) * kPitch + 16 * (t >> 5);
+#pragma unroll
+        for (int rb = 0; rb < NRB; ++rb) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) *reinterpret_cast<bf16x8*>(to + 4 * i * kPitch) = qv[rb][i];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) qv[rb][c] = *reinterpret_cast<const bf16x8*>(from + 32 * c);
+        }
+      }
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) asm volatile("" : "+a"(qv[rb][c]));
       const f32x16 zero = {};
       f32x16 o[NRB][4], s[kBlocks][NRB];                 // O^T, and S^T(j) of the current step [32 keys][row block]
       bf16x8 pb[NRB][2 * kBlocks];                           // P^T(j - 1)
@@ -552,7 +604,6 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
       }
       barrier();                                   // K(0)'s buffer is free
       // buffers of V(j - 1), V(j), V(j + 2), K(j + 1), K(j + 3), and the rows that come next
-      int v_cur = v0, v_next2 = after(after(v0, kVSize, kVBufs), kVSize, kVBufs), v_prev = after(v_next2, kVSize, kVBufs);
       int k_next = after(k0, kKSize, kKBufs), k_next3 = k0;
       const char* kp = u.k + 3 * kStep * (int64_t)kss;
       const char* vp = u.v + 2 * kStep * (int64_t)vss;
@@ -611,21 +662,12 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
             asm volatile("s_nop 1" ::"a"(qv[NRB - 1][0]), "a"(qv[NRB - 1][1]), "a"(qv[NRB - 1][2]), "a"(qv[NRB - 1][3]),
                          "a"(qv[NRB - 1][4]), "a"(qv[NRB - 1][5]), "a"(qv[NRB - 1][6]), "a"(qv[NRB - 1][7]));
           __builtin_amdgcn_sched_barrier(0);
+        } else if (more) {
+          request(un, k_next, after(v_cur, kVSize, kVBufs));
         }
-        // the next unit's loads between the products and the exponentials of this one's last step
-        constexpr int kReq = kPV ? kSlots / 2 : kSlots;
-        const __bf16* q_next;
-        auto spread = [&](auto slot_) {
-          constexpr int slot = decltype(slot_)::value;
-          if constexpr (!kS && slot < kReq) {
-            if (more)
-              each<slot * kPieces / kReq, (slot + 1) * kPieces / kReq>(
-                  [&](auto p) { request(p, q_next, un, k_next, after(v_cur, kVSize, kVBufs)); });
-          }
-        };
         constexpr int i0 = kPV ? 0 : kOps, i1 = kS ? 2 * kOps : kOps;
         if constexpr (!kPV && kS) each<kOps, kOps + kAhead>([&](auto i) { ring[i % kRing] = read(i, vb, kb); });
-        if constexpr (!kPV) each<0, kSlots / 2>([&](auto i) { spread(i); soft(i); });
+        if constexpr (!kPV) each<0, kSlots / 2>([&](auto i) { soft(i); });
         each<i0, i1>([&](auto i) {
           // (behind the last, the first of the next iteration: values of step j)
           if constexpr (i + kAhead < i1)
@@ -644,12 +686,11 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
               mfma_next(sn[(i - kOps) >> 3][rb], ring[i % kRing], qv[rb][i & 7]);
             __builtin_amdgcn_sched_barrier(0);
             soft(std::integral_constant<int, NRB * i + rb>{});
-            spread(std::integral_constant<int, NRB * i + rb>{});
             __builtin_amdgcn_sched_barrier(0);
           });
           if constexpr (kBlocks == 2 && i == kOps + 8) each<0, NRB>([&](auto rb) { kept(sn[0][rb]); });
         });
-        if constexpr (!kS) each<kSlots / 2, kSlots>([&](auto i) { spread(i); soft(i); });
+        if constexpr (!kS) each<kSlots / 2, kSlots>([&](auto i) { soft(i); });
         q0 = p0;
         q1 = p1;
         finish(std::integral_constant<int, kSlots / 2 - 1>{}, 0);
@@ -765,10 +806,12 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
         const Row r = row_of(u, t, rb);
         if (again || !mine) continue;
         const float inv = 1.f / l_tot;
+        const int64_t at = (int64_t)(u.q0 + u.i0) * a.out_st + head0 * a.out_sh;
         auto row = [&](auto* out, int i, bool* ok) {
-          const Row x = row_of(u, (t & ~63) + i, rb);
-          *ok = x.ok;
-          return out + x.row * a.out_st + (int64_t)x.head * a.out_sh;
+          const int x = row0 + 32 * rb + i;
+          const int64_t off = out_off[x];
+          *ok = x < u.cnt * a.rows_head && off >= 0;
+          return out + at + off;
         };
         if (a.out_f32)
           store_block<float>(o[rb], inv, outl[wave], t & 63, [&](int i, bool* ok) { return row((float*)a.out, i, ok); });
@@ -779,7 +822,7 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
       }
       if (again && mine) {
         for (int rb = 0; rb < NRB; ++rb)
-          attend_again((ConstPrefillArgs*)__builtin_amdgcn_kernarg_segment_ptr(), wave % kGroups * (32 * NRB) + 32 * rb, u.q0, u.i0,
+          attend_again((ConstPrefillArgs*)__builtin_amdgcn_kernarg_segment_ptr(), row0 + 32 * rb, u.q0, u.i0,
                        u.cnt, g, hb);
       }
       if (!more) break;
