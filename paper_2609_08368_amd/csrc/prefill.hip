@@ -9,8 +9,8 @@
 // its scores, maximum and sums are in two lanes, and P^T is an operand of the
 // second product as it comes. Four waves, one a SIMD with all 512 registers, of
 // 64 rows each: an operand read from LDS serves two MFMAs (with 32 rows, and
-// eight waves, a 16K prompt of 64 + 8 heads took 4.4 ms against 3.6, bound by
-// those reads). A wave's step is one stream: values of step j - 1, softmax of
+// eight waves, a 16K prompt of 64 + 8 heads took 4.0-4.4 ms against 3.6, bound
+// by those reads). A wave's step is one stream: values of step j - 1, softmax of
 // step j and scores of step j + 1, in which each MFMA is followed by the four or
 // five vector instructions of a softmax slot, which run beside it. Rows of K and
 // V go from memory to LDS by the load, two and three steps ahead, one barrier a
@@ -20,8 +20,8 @@
 // maximum of its first keys, which in 32-bit floats is as good unless a later
 // score is 88 above it. Then a sum or O is infinite or NaN at the end, as it is
 // where a masked value is (0 times infinity), and the wave computes its rows
-// again, slowly and with a running maximum (attend_again). The running maximum
-// costs 7% of a 16K prompt.
+// again, slowly and with a running maximum (attend_again). A running
+// maximum everywhere cost 7-10% of a 16K prompt.
 //
 // Workgroups stay, one a CU, and take units from a longest-first order that each
 // of them works out alike (plan_levels); a unit's first rows are requested in
