@@ -348,7 +348,11 @@ int rl_attn_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const
  *   out        [T, Hq, 128] bf16 (f32 also accepted); lse_out [T, Hq] f32,
  *              nullable. Rows that no prompt owns are left as they were.
  * A row's results depend on no row behind it, whatever that row holds (NaN and
- * infinities included). */
+ * infinities included), and are the same in every call with the same inputs;
+ * their last bits may change with the call's other prompts, which choose how
+ * rows are shared out, and with what lies behind a row where that is not finite.
+ * (Where they must not, rl_attn_extend over appended pages gives rows that are
+ * invariant to their batch.) */
 int rl_attn_prefill(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const rl_tensor* seq_indptr,
                     float scale, rl_tensor* out, rl_tensor* lse_out, void* stream);
 
