@@ -11,7 +11,6 @@ from __future__ import annotations
 import ctypes
 import os
 import re
-import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -130,34 +129,21 @@ def _check(rc: int):
         raise RlAttnError(rc, last_error())
 
 
-_DTYPES = {torch.bfloat16: RL_BF16, torch.float32: RL_F32, torch.int32: RL_I32,
-           torch.float8_e4m3fn: RL_FP8_E4M3, torch.int64: RL_I64}
-
-
-# rl_tensor of 1 to 4 dimensions, the unused shape and stride entries zero
-_LAYOUT = {n: struct.Struct(f"=Qii{n}q{32 - 8 * n}x{n}q{32 - 8 * n}x") for n in range(5)}
-# (the functions behind torch.cuda.current_device() and current_stream(), without what those do besides: 0.1 us
-# instead of 0.2 us for each tensor and 3 us for the stream, of calls whose kernels take 5 us)
+# (the functions behind torch.cuda.current_device() and current_stream(), without what those do besides: 3 us of a
+# call whose kernel takes 5)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                           lambda device: torch.cuda.current_stream(device).cuda_stream)
 
+# The bytes of an rl_tensor describing a tensor (no copy of its data); None -> NULL. The library dereferences the
+# pointers on the current HIP device, so a tensor elsewhere is a ValueError (a host pointer would reach a kernel).
+try:
+    from ._pack import arg as _arg
+except ImportError as e:
+    _arg_missing = e
 
-def _arg(t: Optional[torch.Tensor]) -> Optional[bytes]:
-    """The bytes of an ``rl_tensor`` describing ``t`` (no copy of its data); None -> NULL.
-
-    The library dereferences the pointers on the current HIP device, so every
-    tensor must live there (a host pointer would reach a kernel)."""
-    if t is None:
-        return None
-    device = t.get_device()
-    if device < 0 or device != _current_device():
-        raise ValueError(f"tensor on {t.device}: the library reads and writes tensors on the current device "
-                         f"(cuda:{torch.cuda.current_device() if torch.cuda.is_available() else '?'})")
-    n = t.dim()
-    if n > 4:
-        raise ValueError("rl_tensor holds at most 4 dimensions")
-    return _LAYOUT[n].pack(t.data_ptr(), _DTYPES.get(t.dtype, 0), n, *t.shape, *t.stride())
+    def _arg(t):
+        raise RuntimeError("_pack.so is not built; run __graft_entry__.build() first") from _arg_missing
 
 
 def view(t: Optional[torch.Tensor]):

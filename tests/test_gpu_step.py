@@ -697,3 +697,17 @@ def test_prefill_captured_and_on_another_stream():
         ra.prefill(c["q"], c["k"], c["v"], ptr, 128 ** -0.5, out=want, lse=want_lse)
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(lse[:int(ptr[-1])], want_lse[:int(ptr[-1])]), rep
+
+
+def test_views_describe_tensors():
+    base = torch.zeros(6, 5, 4, 3, device=DEV)
+    for t in (base, base[1:, ::2], base.permute(3, 1, 0, 2), base[2, 3], base[0, 0, 0, 1:], base[0, 0, 0, 0], base[:0],
+              base[:, :1].expand(6, 9, 4, 3), base.to(torch.bfloat16), base.to(torch.int32), base.to(torch.int64),
+              base.to(torch.float8_e4m3fn), base.to(torch.float16)):
+        v, n = ra.view(t), t.dim()
+        dtype = {torch.float32: ra.RL_F32, torch.bfloat16: ra.RL_BF16, torch.int32: ra.RL_I32, torch.int64: ra.RL_I64,
+                 torch.float8_e4m3fn: ra.RL_FP8_E4M3}.get(t.dtype, 0)
+        assert (v.data or 0, v.dtype, v.ndim) == (t.data_ptr(), dtype, n)
+        assert list(v.shape) == [*t.shape] + [0] * (4 - n) and list(v.strides) == [*t.stride()] + [0] * (4 - n)
+    with pytest.raises(ValueError, match="at most 4"):
+        ra.view(base[None])

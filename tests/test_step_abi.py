@@ -193,3 +193,14 @@ def test_calls_of_nothing_are_no_ops():
     for call, args in ((lib.rl_attn_rope, rope_args(T=0)), (lib.rl_attn_rope_append_kv, append_args(False, T=0)),
                        (lib.rl_attn_prefill, prefill_args(T=0)), (lib.rl_attn_prefill, prefill_args(B=0))):
         assert call(*(ref(a) for a in args.values()), None) == 0, ra.last_error()
+
+
+def test_a_tensor_is_described_or_refused():
+    """(on a GPU too, in the tests that run there)"""
+    import torch
+
+    assert ra.view(None) is None
+    with pytest.raises(ValueError, match="tensor on cpu: .* current device"):
+        ra.view(torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(TypeError, match="expected a tensor or None, got list"):
+        ra.view([1, 2])
