@@ -45,7 +45,7 @@ namespace {
 
 constexpr int kPreThreads = 256;       // four waves, one a SIMD
 constexpr int kStep = 64;              // keys of a step
-constexpr int kAhead = 4, kRing = 8;   // LDS operands read ahead of their MFMAs, and their registers
+constexpr int kAhead = 4, kRing = 8;   // LDS operands read ahead of a pair's MFMAs, and their registers
 constexpr int kKPitch = 1024 + 16;     // LDS blocks of four 256-byte rows
 constexpr int kVPitch = 1024 + 64;
 constexpr int kKSize = 16 * kKPitch, kVSize = 16 * kVPitch;
@@ -670,10 +670,20 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
         if constexpr (!kPV) each<0, kSlots / 2>([&](auto i) { soft(i); });
         each<i0, i1>([&](auto i) {
           // (behind the last, the first of the next iteration: values of step j)
-          if constexpr (i + kAhead < i1)
-            ring[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead>{}, vb, kb);
-          else
-            ring[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead - i1>{}, vb_next, kb);
+          // Two at a time, with one wait for both (17 waits a step instead of 33: 0.7% of a 16K prompt, 4% of short steps;
+          // four at a time spilled registers): the counter falls in order, and behind the second are the reads of the
+          // next four operands (two for one of V).
+          if constexpr ((i & 1) == 0) {
+            each<i + kAhead, i + kAhead + 2>([&](auto k) {
+              if constexpr (k < i1)
+                ring[k % kRing] = read(k, vb, kb);
+              else
+                ring[k % kRing] = read(std::integral_constant<int, k - i1>{}, vb_next, kb);
+            });
+            constexpr auto reads = [](int k) { return k % i1 >= i0 && k % i1 < kOps ? 2 : 1; };
+            constexpr int behind = reads(i + 2) + reads(i + 3) + reads(i + 4) + reads(i + 5);
+            __builtin_amdgcn_s_waitcnt(0xc07f | behind << 8);
+          }
           __builtin_amdgcn_sched_barrier(0);
           each<0, NRB>([&](auto rb) {
             if constexpr (i < kOps)
