@@ -20,8 +20,10 @@
 // maximum of its first keys, which in 32-bit floats is as good unless a later
 // score is 88 above it. Then a sum or O is infinite or NaN at the end, as it is
 // where a masked value is (0 times infinity), and the wave computes its rows
-// again, slowly and with a running maximum (attend_again). A running
-// maximum everywhere cost 7-10% of a 16K prompt.
+// again, slowly and with a running maximum (attend_again). Where two waves split
+// a tile's keys, each has such a maximum of its own, and the weights that join
+// them are kept in range whatever the distance of the two. A running maximum
+// everywhere cost 7-10% of a 16K prompt.
 //
 // Workgroups stay, one a CU, and take units from a longest-first order that each
 // of them works out alike (plan_levels); a unit's first rows are requested in
@@ -791,10 +793,14 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
           }
           barrier_lds();
           if (part == 0) {
+            // The bases are of the first keys only, so a sum may be up to 2^128 times its part's weight and the lower
+            // part still count where 2^(m0 - m1) is flushed to zero (below 2^-126). Far parts are joined 2^96 higher,
+            // where it is not down to a distance of 222 (and a part that much lower does not count).
             const float l1 = ml[0], m0 = -nm[rb], m1 = l1 == 0.f ? kNegInf : ml[1], m = fmaxf(m0, m1);
-            const float w0 = exp2_fast(m0 - m), w1 = exp2_fast(m1 - m);
+            const float up = l1 != 0.f && m - fminf(m0, m1) > 120.f ? 96.f : 0.f;
+            const float w0 = exp2_fast(m0 - m + up), w1 = exp2_fast(m1 - m + up);
             l[rb] = l[rb] * w0 + (kg ? 0.f : l1 * w1);
-            nm[rb] = -m;
+            nm[rb] = up - m;
 #pragma unroll
             for (int jd = 0; jd < 4; ++jd)
 #pragma unroll
