@@ -795,11 +795,12 @@ __device__ __forceinline__ void tile_attend_dl(const PagedKV& kv, float scale, c
     // rows' readers are ordered by wait_loads and the barriers instead; a wait
     // the compiler counts for its own loads can only be lengthened by these
     // (loads complete in order).
-    // (m0 holds the LDS address: an input operand, so the compiler sets it)
+    // (m0 holds the LDS address: an input operand, so the compiler sets it, as late as right before the statement,
+    // which it does not know as a load: the wait state between the two stands here)
     if constexpr (kNt)
-      asm volatile("global_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(sbase), "{m0}"(lds) : "memory");
+      asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(sbase), "{m0}"(lds) : "memory");
     else
-      asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds) : "memory");
+      asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds) : "memory");
   };
   auto dma = [&](int j, const int (&p)[2], const char* base, int64_t sp, uint32_t ss, char* dst, int pitch) {
 #pragma unroll
