@@ -20,7 +20,8 @@
 // maximum of its first keys, which in 32-bit floats is as good unless a later
 // score is 88 above it. Then a sum or O is infinite or NaN at the end, as it is
 // where a masked value is (0 times infinity), and the wave computes its rows
-// again, slowly and with a running maximum (attend_again). Where two waves split
+// again, slowly and with a running maximum (attend_again); so it does where a sum
+// is below 1/2, which scores of 1e7 and more can do. Where two waves split
 // a tile's keys, each has such a maximum of its own, and the weights that join
 // them are kept in range whatever the distance of the two. A running maximum
 // everywhere cost 7-10% of a 16K prompt.
@@ -240,7 +241,10 @@ __device__ __forceinline__ bool odd_values(const f32x16 (&o)[NRB][4], const floa
 
 // A block of 32 rows of a unit (row r0 on) again, without the two shortcuts of the
 // fast path: the running maximum follows every step, and a masked key's value
-// takes no part at all (0 times an infinity or a NaN is NaN). By one wave, operands
+// takes no part at all (0 times an infinity or a NaN is NaN). Its maximum is of
+// the raw scores and subtracted before the scale, which is exact for the largest
+// one: minus a scaled and rounded maximum, a score of 1e10 powers of two would
+// leave hundreds of them. By one wave, operands
 // straight from memory; keys below `whole`, which every row sees, by MFMA, the
 // others one by one. Not inlined: the fast path's registers are its own.
 typedef __attribute__((address_space(4))) const PrefillArgs ConstPrefillArgs;
@@ -260,7 +264,7 @@ __device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int
   const float sl2 = a.scale * kLog2e;
   const f32x16 zero = {};
   f32x16 o[4] = {zero, zero, zero, zero};
-  float m = kNoKey, l = 0.f;
+  float m = -__FLT_MAX__, l = 0.f;
 #pragma unroll 1
   for (int t0 = 0; t0 < whole; t0 += 32) {
     f32x16 s = zero;
@@ -270,7 +274,7 @@ __device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int
     float mx = s[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-    const float m_new = fmaxf(m, max_l32(mx) * sl2), alpha = exp2_fast(m - m_new);
+    const float m_new = fmaxf(m, max_l32(mx)), alpha = exp2_fast((m - m_new) * sl2);
     m = m_new;
     l *= alpha;
 #pragma unroll
@@ -280,7 +284,7 @@ __device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int
       bf16x8 p;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = exp2_fast(fmaf(s[8 * h + e], sl2, -m));
+        const float x = exp2_fast((s[8 * h + e] - m) * sl2);
         l += x;
         p[e] = (__bf16)x;
       }
@@ -305,9 +309,9 @@ __device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int
 #pragma unroll
       for (int e = 0; e < 8; ++e) s = fmaf((float)x[e], (float)qv[c][e], s);
     }
-    s = sum_l32(s) * sl2;
+    s = sum_l32(s);
     if (t > limit) continue;
-    const float m_new = fmaxf(m, s), alpha = exp2_fast(m - m_new), p = exp2_fast(s - m_new);
+    const float m_new = fmaxf(m, s), alpha = exp2_fast((m - m_new) * sl2), p = exp2_fast((s - m_new) * sl2);
     m = m_new;
     l = l * alpha + (kg ? 0.f : p);
 #pragma unroll
@@ -324,7 +328,7 @@ __device__ __attribute__((noinline)) void attend_again(ConstPrefillArgs* ap, int
   else
     store_o_row((__bf16*)a.out + row * a.out_st + (int64_t)head * a.out_sh, o, inv);
   if (a.lse && lane < 32)
-    a.lse[row * a.lse_st + (int64_t)head * a.lse_sh] = (m + __builtin_amdgcn_logf(l_tot)) * kLn2;
+    a.lse[row * a.lse_st + (int64_t)head * a.lse_sh] = fmaf(m, sl2, __builtin_amdgcn_logf(l_tot)) * kLn2;
 }
 
 // A wave's 32 rows to memory. O^T has a row's dimensions in two lanes, four
@@ -782,7 +786,10 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
         for (int rb = 0; rb < NRB; ++rb) {
           barrier_lds();
           if (part == 1) {
-            ml[0] = sum_l32(l[rb]);
+            const Row r = row_of(u, here(tid), rb);
+            const bool sees = (r.ok ? u.i0 + r.ti : u.keys - 1) >= 32;
+            const float l1 = sum_l32(l[rb]);
+            ml[0] = sees && l1 < 0.5f ? -kNegInf : l1;   // (see below: again)
             ml[1] = -nm[rb];
 #pragma unroll
             for (int jd = 0; jd < 4; ++jd)
@@ -814,11 +821,19 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
       }
       const int t = here(tid);
       const bool mine = kParts == 1 || part == 0;  // these rows are this wave's to store
-      const bool again = __builtin_amdgcn_ballot_w64(odd_values<NRB>(o, l)) != 0;
+      bool odd = false;
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb) {
+        l[rb] = sum_l32(l[rb]);
+        // The first keys' maximum has a probability of 1 but for its rounding. That is half a power of two from 2^24
+        // powers on and past all of them from 2^32 on, where nothing may be left of a sum.
+        odd |= l[rb] < 0.5f;
+      }
+      const bool again = __builtin_amdgcn_ballot_w64(odd || odd_values<NRB>(o, l)) != 0;
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the next unit's rows have come (before the stores, which need not)
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb) {
-        const float l_tot = sum_l32(l[rb]);
+        const float l_tot = l[rb];
         const Row r = row_of(u, t, rb);
         if (again || !mine) continue;
         const float inv = 1.f / l_tot;
