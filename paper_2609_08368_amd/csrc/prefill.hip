@@ -72,7 +72,8 @@ __device__ __forceinline__ void each(F&& f) {
 // kernel into AGPRs and copy the scores out of them, an instruction for each. It
 // does not know these as MFMAs, so what their hazards ask for is done by hand:
 // q is in place two instructions before the first (body), and no result is read
-// before 11 wait states after the last (body, and the scores' first use).
+// before 12 wait states after the last (body, and the scores' first use), which
+// is what the compiler leaves behind the same product as a builtin.
 __device__ __forceinline__ void mfma_first(f32x16& c, const bf16x8& a, const bf16x8& b) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "a"(b));
 }
