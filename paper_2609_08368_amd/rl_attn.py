@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import warnings
 from typing import NamedTuple, Optional
 
 import torch
@@ -135,15 +136,44 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                           lambda device: torch.cuda.current_stream(device).cuda_stream)
 
-# The bytes of an rl_tensor describing a tensor (no copy of its data); None -> NULL. The library dereferences the
-# pointers on the current HIP device, so a tensor elsewhere is a ValueError (a host pointer would reach a kernel).
-try:
-    from ._pack import arg as _arg
-except ImportError as e:
-    _arg_missing = e
+_DTYPES = {torch.bfloat16: RL_BF16, torch.float32: RL_F32, torch.int32: RL_I32, torch.int64: RL_I64,
+           torch.float8_e4m3fn: RL_FP8_E4M3}
+_PACK_PATH = os.path.join(_PKG, "_pack.so")
 
-    def _arg(t):
-        raise RuntimeError("_pack.so is not built; run __graft_entry__.build() first") from _arg_missing
+
+def _describe(t):
+    """The bytes of an rl_tensor describing a tensor (no copy of its data); None -> NULL. The library dereferences the
+    pointers on the current HIP device, so a tensor elsewhere is a ValueError (a host pointer would reach a kernel)."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"expected a tensor or None, got {type(t).__name__}")
+    if not t.is_cuda or t.device.index != _current_device():
+        raise ValueError(f"tensor on {t.device}: the library reads and writes tensors on the current device")
+    if t.dim() > 4:
+        raise ValueError("rl_tensor holds at most 4 dimensions")
+    v = RlTensor()
+    v.data, v.dtype, v.ndim = t.data_ptr() or None, _DTYPES.get(t.dtype, 0), t.dim()
+    v.shape[:v.ndim], v.strides[:v.ndim] = t.shape, t.stride()
+    return bytes(v)
+
+
+def _first_arg(t):
+    """`_describe` by the compiled module, from the first call that finds it on (0.1 us a tensor instead of 3); without
+    one that loads here (not built, or for another Python or torch) calls work all the same."""
+    global _arg
+    if os.path.exists(_PACK_PATH):
+        try:
+            from ._pack import arg as _arg
+        except ImportError as e:
+            warnings.warn(f"{_PACK_PATH} does not load, tensors are described in Python (slower): {e}", RuntimeWarning,
+                          stacklevel=3)
+            _arg = _describe
+        return _arg(t)
+    return _describe(t)
+
+
+_arg = _first_arg
 
 
 def view(t: Optional[torch.Tensor]):
