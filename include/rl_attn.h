@@ -256,7 +256,12 @@ int rl_attn_append_kv_fp8(const rl_tensor* k_new, const rl_tensor* v_new, const 
 /* ---- a step's rows: where they go, their positions, their first attention ----
  * An engine's step is rl_attn_map_slots, then per layer rl_attn_rope_append_kv
  * and rl_attn_prefill (first turns), rl_attn_extend (later ones) or
- * rl_attn_decode. */
+ * rl_attn_decode. What these calls write may be what they read only where that
+ * is said, as the same view; otherwise no output may overlap itself, another
+ * output or an input. Lengths, tables, rows and log-sum-exps that do are refused
+ * (views of one buffer that share no byte are apart if they have the same
+ * strides); that pages, positions and slots are apart from them is the
+ * caller's part. */
 
 /* Slot maps (paper: every turn appends its suffix to cached context, section
  * "Fast Agentic Rollout with SGLang"): from the lengths of a step's requests,
@@ -272,8 +277,7 @@ int rl_attn_append_kv_fp8(const rl_tensor* k_new, const rl_tensor* v_new, const 
  *   block_table [B, max_pages] int32: its entries for c_b cached tokens are
  *              read, those of new pages are written, no other is touched
  *   kv_lens_out [B], free_used_out [1] int32: c_b + n_b, and the entries now
- *              taken; may be kv_lens and free_used themselves (a step in place),
- *              else must not overlap them
+ *              taken; may be kv_lens and free_used themselves (a step in place)
  *   qo_indptr  [B+1] int32: row bounds, qo_indptr[b+1] - qo_indptr[b] = n_b
  *   slot_map   [T] int64, T >= sum of n_b: page * page_size + slot in the page
  *              of each row; -1 in the rows behind the last request's
@@ -309,8 +313,7 @@ typedef struct {
  *   axes       [F] int32: the axis (row of positions) of each frequency, e.g.
  *              time, height and width in blocks or in turn; NULL for A = 1. An
  *              axis outside [0, A) is clamped and reported.
- *   q_out, k_out: as q and k, and may be q and k (the same view); they must not
- *              overlap them otherwise */
+ *   q_out, k_out: as q and k, and may be q and k (the same view) */
 int rl_attn_rope(const rl_tensor* q, const rl_tensor* k, const rl_tensor* positions, const rl_tensor* inv_freq,
                  const rl_tensor* axes, const rl_rope_opts* opts, rl_tensor* q_out, rl_tensor* k_out, void* stream);
 
@@ -345,8 +348,9 @@ int rl_attn_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const
  *   k, v       [T, Hkv, 128] bf16 (row strides below 2^24 elements)
  *   seq_indptr [B+1] int32: prompt b owns rows seq_indptr[b] .. seq_indptr[b+1]-1;
  *              bounds that decrease or leave [0, T] are clamped and reported
- *   out        [T, Hq, 128] bf16 (f32 also accepted); lse_out [T, Hq] f32,
- *              nullable. Rows that no prompt owns are left as they were.
+ *   out        [T, Hq, 128] bf16 (f32 also accepted), may be q (the same view);
+ *              lse_out [T, Hq] f32, nullable. Rows that no prompt owns are left
+ *              as they were.
  * A row's results depend on no row behind it, whatever that row holds (NaN and
  * infinities included), and are the same in every call with the same inputs;
  * their last bits may change with the call's other prompts, which choose how

@@ -142,6 +142,95 @@ int check_rows128(const rl_tensor* t, const char* name) {
   return RL_OK;
 }
 
+int64_t elem_bytes(int dtype) {
+  return dtype == RL_I64 ? 8 : dtype == RL_BF16 ? 2 : dtype == RL_FP8_E4M3 ? 1 : 4;
+}
+
+// The bytes of a view of up to two dimensions of runs: n0 x n1 runs of `width` bytes. (A last dimension of 128 with
+// stride 1 is a run.)
+struct Runs {
+  intptr_t at;
+  int64_t n0, s0, n1, s1, width;
+};
+Runs runs_of(const rl_tensor* t) {
+  const int64_t e = elem_bytes(t->dtype);
+  Runs r{reinterpret_cast<intptr_t>(t->data), 1, 0, 1, 0, e};
+  const int n = t->ndim == 3 ? 2 : t->ndim;         // (three dimensions: rows, heads, 128)
+  if (t->ndim == 3) r.width = e * t->shape[2];
+  if (n > 0) r.n0 = t->shape[0], r.s0 = e * t->strides[0];
+  if (n > 1) r.n1 = t->shape[1], r.s1 = e * t->strides[1];
+  return r;
+}
+
+// Whether two views (or, with self, two runs of one) share a byte. Exact where their strides are the same, as those of
+// slices of one buffer are; views of other strides are taken to meet where their ranges do.
+bool runs_meet(Runs a, Runs b, bool self) {
+  if (a.n0 < 1 || a.n1 < 1 || b.n0 < 1 || b.n1 < 1) return false;
+  auto end = [](const Runs& r) { return r.at + (r.n0 - 1) * r.s0 + (r.n1 - 1) * r.s1 + r.width; };
+  if (a.at >= end(b) || b.at >= end(a)) return false;
+  if (a.n0 == 1) a.s0 = b.s0;
+  if (b.n0 == 1) b.s0 = a.s0;
+  if (a.n1 == 1) a.s1 = b.s1;
+  if (b.n1 == 1) b.s1 = a.s1;
+  if (a.s0 != b.s0 || a.s1 != b.s1) return true;
+  // mostly a row's runs lie within a row's stride (a dense view, slices of one buffer) and those of both in parts of it
+  const int64_t row_a = (a.n1 - 1) * a.s1 + a.width, row_b = (b.n1 - 1) * b.s1 + b.width;
+  if (a.s0 > 0 && row_a <= a.s0 && row_b <= a.s0) {
+    if (self) return a.n1 > 1 && a.s1 < a.width;
+    const int64_t d = (a.at - b.at) % a.s0, off = d < 0 ? d + a.s0 : d;
+    if (off >= row_b && off + row_a <= a.s0) return false;
+  }
+  if (a.n0 + b.n0 < a.n1 + b.n1) {                  // (the loop goes over the second dimension)
+    std::swap(a.n0, a.n1), std::swap(a.s0, a.s1);
+    std::swap(b.n0, b.n1), std::swap(b.s0, b.s1);
+  }
+  // runs i0, i1 of a and j0, j1 of b are at - b.at + (i0 - j0) s0 + (i1 - j1) s1 bytes apart
+  for (int64_t d1 = 1 - b.n1; d1 < a.n1; ++d1) {
+    const int64_t c = a.at - b.at + d1 * a.s1;
+    int64_t lo = 1 - b.n0, hi = a.n0 - 1;           // of d0 with -a.width < c + d0 s0 < b.width
+    if (a.s0 > 0) {
+      auto floor_div = [](int64_t x, int64_t y) { return x / y - (x % y < 0); };
+      lo = std::max(lo, floor_div(-a.width - c, a.s0) + 1);
+      hi = std::min(hi, -floor_div(c - b.width, a.s0) - 1);
+    } else if (c <= -a.width || c >= b.width) {
+      continue;
+    }
+    if (lo <= hi && !(self && d1 == 0 && lo == 0 && hi == 0)) return true;
+  }
+  return false;
+}
+
+struct Named {
+  const rl_tensor* t;
+  const char* name;
+};
+// Written views must not overlap themselves, each other, or what the call reads, except that `outs[i]` may be
+// `same[i]` (the same view).
+int check_apart(const Named* outs, const rl_tensor* const* same, int n_outs, const Named* ins, int n_ins) {
+  for (int i = 0; i < n_outs; ++i) {
+    if (!outs[i].t) continue;
+    const Runs x = runs_of(outs[i].t);
+    if (runs_meet(x, x, true))
+      return fail(RL_ERR_UNSUPPORTED, "%s: elements that are written must not overlap", outs[i].name);
+    for (int j = i + 1; j < n_outs; ++j)
+      if (outs[j].t && runs_meet(x, runs_of(outs[j].t), false))
+        return fail(RL_ERR_UNSUPPORTED, "%s and %s must not overlap", outs[i].name, outs[j].name);
+    for (int j = 0; j < n_ins; ++j) {
+      if (!ins[j].t) continue;
+      const Runs y = runs_of(ins[j].t);
+      const bool may = same[i] == ins[j].t;
+      auto stride = [](int64_t n, int64_t s) { return n > 1 ? s : 0; };
+      if (may && x.at == y.at && x.width == y.width && x.n0 == y.n0 && x.n1 == y.n1 &&
+          stride(x.n0, x.s0) == stride(y.n0, y.s0) && stride(x.n1, x.s1) == stride(y.n1, y.s1))
+        continue;
+      if (runs_meet(x, y, false))
+        return fail(RL_ERR_UNSUPPORTED, may ? "%s must be %s or not overlap it" : "%s and %s must not overlap",
+                    outs[i].name, ins[j].name);
+    }
+  }
+  return RL_OK;
+}
+
 // The kernels take the row maximum of raw scores and fold the scale into the
 // exponent, which needs a positive, finite scale.
 int check_scale(float scale) {
@@ -1047,6 +1136,12 @@ int map_impl(const rl_tensor* kv_lens, const rl_tensor* new_lens, const rl_tenso
   if (rows > INT32_MAX / 2) return fail(RL_ERR_UNSUPPORTED, "slot map too long");
   RL_TRY(check_vector(slot_map, "slot_map", RL_I64, rows, true));
   RL_TRY(check_vector(positions, "positions", RL_I32, rows, true));
+  const Named outs[] = {{block_table, "block_table"}, {kv_lens_out, "kv_lens_out"}, {free_used_out, "free_used_out"},
+                        {qo_indptr, "qo_indptr"}, {slot_map, "slot_map"}, {positions, "positions"}};
+  const rl_tensor* same[] = {nullptr, kv_lens, free_used, nullptr, nullptr, nullptr};
+  const Named ins[] = {{kv_lens, "kv_lens"}, {new_lens, "new_lens"}, {free_pages, "free_pages"},
+                       {free_used, "free_used"}, {pos_delta, "pos_delta"}};
+  RL_TRY(check_apart(outs, same, 6, ins, 5));
   hipStream_t st = static_cast<hipStream_t>(stream);
   Workspace* w = nullptr;
   RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
@@ -1191,6 +1286,9 @@ int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const 
     a.v_sh = v->strides[1];
   }
   if (rows == 0 || Hq + Hkv == 0) return RL_OK;
+  const Named outs[] = {{q_out, "q_out"}, {k_out, "k_out"}}, ins[] = {{q, "q"}, {k, k_name}, {v, "v_new"}};
+  const rl_tensor* same[] = {q, k};
+  RL_TRY(check_apart(outs, same, 2, ins, 3));
   int cus = 0;
   RL_TRY(current_cus(&cus));
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -1265,6 +1363,9 @@ int prefill_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, con
     return fail(RL_ERR_UNSUPPORTED, "k/v: row strides must be < 2^24 elements");
   RL_TRY(check_data(q, "q"));
   if (B == 0 || rows == 0) return RL_OK;
+  const Named outs[] = {{out, "out"}, {lse_out, "lse_out"}}, ins[] = {{q, "q"}, {k, "k"}, {v, "v"}};
+  const rl_tensor* same[] = {q, nullptr};
+  RL_TRY(check_apart(outs, same, 2, ins, 3));
   rl::PrefillArgs a{};
   int cus = 0;
   RL_TRY(current_cus(&cus));
