@@ -38,8 +38,6 @@ def compiler() -> list:
         # reaches the output through the exponent), so fmaxf needs no NaN-quieting
         # canonicalisation; the host code keeps full NaN semantics
         "-Xarch_device", "-fno-honor-nans",
-        # statements that set m0 say so, which is warned of (the compiler keeps nothing there)
-        "-Wno-inline-asm",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC,
     ]
 

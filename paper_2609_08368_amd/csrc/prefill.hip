@@ -425,7 +425,10 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
     }
     // As assembly: see the 128-key routine in tile_attn.hpp. In one statement, since
     // the compiler does not know it as loads: an SGPR that a vector instruction
-    // wrote (the reload of a spilled one) needs 5 wait states, and m0 needs 1.
+    // wrote (the reload of a spilled one) needs 5 wait states, and m0 needs 1. It
+    // says that it sets m0, of which the compiler warns (it keeps nothing there).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
     asm volatile(
         "s_mov_b32 m0, %5\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %4\n\t"
         "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %4\n\t"
@@ -433,6 +436,7 @@ __global__ __launch_bounds__(kPreThreads, 1) void prefill_kernel(PrefillArgs a) 
         "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4" ::"v"(at[0]),
         "v"(at[1]), "v"(at[2]), "v"(at[3]), "s"(rows), "s"(lds), "i"(kPitch)
         : "memory", "m0", "scc");
+#pragma clang diagnostic pop
   };
   auto barrier = [&]() {
     asm volatile("" ::: "memory");
