@@ -90,23 +90,32 @@ __device__ __forceinline__ Chunks chunks_of(int d, int F, bool interleaved) {
   return {16 * d, 16 * d + 8, turned};
 }
 
-// cs: cos and sin of the duplet's eight frequencies
+// cs: cos and sin of the duplet's eight frequencies. (x cos a - y sin a, y cos a +
+// x sin a), with the fused products written out: left to the compiler they differ
+// between the kernels, and a row's bits with the size of its call.
+__device__ __forceinline__ void turn_pair(float& x, float& y, float2 cs) {
+  const float u = x, w = y;
+  x = fmaf(u, cs.x, -(w * cs.y));
+  y = fmaf(w, cs.x, u * cs.y);
+}
 __device__ __forceinline__ void turn(f32x8& a, f32x8& b, const float2 (&cs)[8], bool interleaved) {
   if (interleaved) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      f32x8& x = e < 4 ? a : b;
+      f32x8& z = e < 4 ? a : b;
       const int i = 2 * (e & 3);
-      const float u = x[i], w = x[i + 1];
-      x[i] = u * cs[e].x - w * cs[e].y;
-      x[i + 1] = w * cs[e].x + u * cs[e].y;
+      float x = z[i], y = z[i + 1];
+      turn_pair(x, y, cs[e]);
+      z[i] = x;
+      z[i + 1] = y;
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float u = a[e], w = b[e];
-      a[e] = u * cs[e].x - w * cs[e].y;
-      b[e] = w * cs[e].x + u * cs[e].y;
+      float x = a[e], y = b[e];
+      turn_pair(x, y, cs[e]);
+      a[e] = x;
+      b[e] = y;
     }
   }
 }
