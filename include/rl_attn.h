@@ -356,7 +356,11 @@ int rl_attn_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const
  * their last bits may change with the call's other prompts, which choose how
  * rows are shared out, and with what lies behind a row where that is not finite.
  * (Where they must not, rl_attn_extend over appended pages gives rows that are
- * invariant to their batch.) */
+ * invariant to their batch.) Probabilities are rounded to bf16 before they weigh
+ * the values, whatever the type of out: 2^-8 of the mean magnitude of the values
+ * that a row sees, at most. Scores may have any size that float32 holds; rows with
+ * a score 88 above those of their first 32 keys (or beyond 1e7), and rows beside
+ * a value that is not finite, are computed twice, the second time slowly. */
 int rl_attn_prefill(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const rl_tensor* seq_indptr,
                     float scale, rl_tensor* out, rl_tensor* lse_out, void* stream);
 

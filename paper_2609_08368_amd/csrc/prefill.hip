@@ -24,18 +24,35 @@
 // is below 1/2, which scores of 1e7 and more can do. Where two waves split
 // a tile's keys, each has such a maximum of its own, and the weights that join
 // them are kept in range whatever the distance of the two. A running maximum
-// everywhere cost 7-10% of a 16K prompt.
+// everywhere cost 7-10% of a 16K prompt. The second attempt is dear: with all rows
+// of prompts of 300 to 16384 a call takes 7.6-8.7 times as long, and a lone wave's
+// 64 rows with 4K (16K) keys, as for an infinity in the last value, add 0.7 ms
+// (3.3 ms) to it.
+//
+// Probabilities are rounded to bf16 for the second product, as in the extend
+// kernels: the MFMAs that keep 32 bits run at a fraction of the rate, and two bf16
+// halves would be half as many MFMAs again. A result is off by 2^-8 of the mean
+// magnitude of its values at most, as much as its own rounding to bf16 (rms of the
+// two together 2.1e-3, of the rounding alone 1.6e-3), also where the output has 32
+// bits. Row sums are of the unrounded ones, in 32 bits.
 //
 // Workgroups stay, one a CU, and take units from a longest-first order that each
 // of them works out alike (plan_levels); a unit's first rows are requested in
 // the last step of the one before.
 //
-// MFMA-bound: a 16384-row prompt of 64 + 8 heads runs at 1.20-1.25 PFLOP/s
-// (3.5-3.7 ms, box to box; a large bf16 matrix product of the library runs at
-// 1.22), a step of 256 rows in 3200 cycles where its MFMAs alone take 2048. Short
-// prompts pay a unit's 9,000 cycles around its steps (operands and scores of the
-// first one, the last values, rows out): 24 prompts of up to 701 rows of 96 + 8
-// heads run at 0.47 PFLOP/s (221 us, 2.1 TB/s).
+// MFMA-bound: a 16384-row prompt of 64 + 8 heads runs at 1.20-1.27 PFLOP/s
+// (3.45-3.67 ms, box to box; a large bf16 matrix product of the library runs at
+// 1.22). Its cycles and those of 16 prompts of 2-4K rows are 3,130 a step of 256
+// rows, of which the MFMAs take 2,048, and 20,000 a unit around the steps
+// (operands and scores of the first one, the last values, rows out, and what the
+// CUs wait for each other at the end). With 4.5 steps a unit that is most of it:
+// 24 prompts of up to 701 rows of 96 + 8 heads run at 0.49-0.51 PFLOP/s (202-213
+// us, 2.1-2.3 TB/s), MFMAs busy 24%.
+//
+// The grid is a multiple of the head groups (KV heads times blocks of query
+// heads), since a unit's order is worked out for one: of 256 CUs, 96 groups use
+// 192 and 129 use 129 (2000 rows of 128 heads of their own take 157 us, of 129
+// 254).
 #include <algorithm>
 #include <type_traits>
 

@@ -1370,8 +1370,8 @@ int prefill_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, con
   int cus = 0;
   RL_TRY(current_cus(&cus));
   // The largest tile that gives every CU a unit, as far as the sizes tell (half a tile more a prompt). One prompt of
-  // 4095 rows of 8 + 2 heads took 97 us in tiles of 256, 68 of 128 and 59 of 64; of 8192 rows 190, 152 and 194; of
-  // 4095 rows of 32 + 8 heads 135, 162 and 201; four of 300 rows of 64 + 8 heads 30, 38 and 36.
+  // 4095 rows of 8 + 2 heads takes 93 us in tiles of 256, 65 of 128 and 52 of 64; of 8192 rows 182, 144 and 181; of
+  // 4095 rows of 32 + 8 heads 127, 155 and 197; four of 300 rows of 64 + 8 heads 25, 38 and 37.
   const int64_t R = Hq / Hkv;
   auto few = [&](int tile_rows) {
     const ExtendShape x = extend_shape(R, tile_rows);
