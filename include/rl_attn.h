@@ -341,6 +341,151 @@ int rl_attn_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const
                                rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, const rl_tensor* k_scale,
                                const rl_tensor* v_scale, void* stream);
 
+/* Models that norm the queries and keys of each head: rl_attn_rope and
+ * rl_attn_rope_append_kv(_fp8) with the norm in the same pass. A head's row x of
+ * q or k becomes x (mean(x^2) + eps)^(-1/2) w before it is rotated; values are
+ * not normed.
+ *   q_weight, k_weight [128], both bf16 or both f32 (k_weight NULL where k is)
+ *   eps        positive and finite, not subnormal
+ * Everything is formed in 32 bits and rounded once, at the end (a model that
+ * rounds the normed row to bf16 before it rotates differs by that rounding). A
+ * row whose squares sum past 2^128 is taken as infinitely long. All else is as for
+ * the calls without a norm (opts.inverse must be 0). */
+int rl_attn_norm_rope(const rl_tensor* q, const rl_tensor* k, const rl_tensor* q_weight, const rl_tensor* k_weight,
+                      float eps, const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                      const rl_rope_opts* opts, rl_tensor* q_out, rl_tensor* k_out, void* stream);
+
+int rl_attn_norm_rope_append_kv(const rl_tensor* q, const rl_tensor* k_new, const rl_tensor* v_new,
+                                const rl_tensor* q_weight, const rl_tensor* k_weight, float eps,
+                                const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                                const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out,
+                                rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, void* stream);
+
+int rl_attn_norm_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const rl_tensor* v_new,
+                                    const rl_tensor* q_weight, const rl_tensor* k_weight, float eps,
+                                    const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                                    const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out,
+                                    rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, const rl_tensor* k_scale,
+                                    const rl_tensor* v_scale, void* stream);
+
+/* The gradient of rl_attn_norm_rope (the trainer's side of the same rows):
+ *   dq_out, dk_out [T, H, 128] bf16: gradients of q_out and k_out
+ *   q, k, weights, eps, positions, inv_freq, axes, opts: as in the forward call
+ *   dq, dk     [T, H, 128] bf16, written; may be dq_out and dk_out (the same view)
+ *   dq_weight, dk_weight [128] f32, written: sums over all rows and heads, in one
+ *              order: the same call gives the same bits
+ * dk_out, dk and dk_weight are NULL where k is. Needs
+ * rl_attn_norm_rope_backward_workspace_size() bytes of workspace. */
+int rl_attn_norm_rope_backward(const rl_tensor* dq_out, const rl_tensor* dk_out, const rl_tensor* q,
+                               const rl_tensor* k, const rl_tensor* q_weight, const rl_tensor* k_weight, float eps,
+                               const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                               const rl_rope_opts* opts, rl_tensor* dq, rl_tensor* dk, rl_tensor* dq_weight,
+                               rl_tensor* dk_weight, void* stream);
+size_t rl_attn_norm_rope_backward_workspace_size(void);
+
+/* ---- what a step answers ---- */
+
+/* Log probabilities of given tokens (paper: rollouts come with the log
+ * probabilities that the trainer's are compared with, section "Case Study"), with
+ * the entropy of the distribution and its likeliest tokens. With z = row_scale[t]
+ * logits[t]: lse = ln sum_j exp z_j, logprob = z_token - lse, entropy = lse -
+ * sum_j p_j z_j.
+ *   logits     [T, V] bf16 or f32, V <= 2^21, last stride 1, any row stride (views
+ *              of a wider buffer, rows that start at any element)
+ *   tokens     [T] int32 or int64. A row with a negative token is left out: its
+ *              logits are not read, its outputs are 0, its alternatives -1 and
+ *              -inf. A token of V or more is reported and its row left out.
+ *   row_scale  [T] f32, nullable (1): e.g. one over a temperature, any stride from
+ *              0 on; must be positive and finite, else the row is reported and left out
+ *   logprobs   [T] f32; entropy, lse [T] f32, nullable
+ *   top_ids    [T, K] int32, top_logprobs [T, K] f32, K <= 32, both nullable: the K
+ *              likeliest tokens, larger logits first, of equal ones the lower index;
+ *              -1 and -inf where fewer than K tokens have a logit above -inf
+ * Logits of -inf exclude tokens (log probability -inf); a row of nothing else has
+ * lse = logprob = -inf and entropy 0. A row with a NaN or +inf gives NaN, and its
+ * alternatives are those among the others and +inf. A row's bits
+ * depend on its own logits, token and scale alone: not on the other rows of the
+ * call, its size, or where the row lies (section "True-On-Policy Alignment" asks
+ * for batch invariance). Calls of fewer rows than 8 a compute unit need
+ * rl_attn_token_logprobs_workspace_size bytes of workspace (top = K or 0); the size
+ * does not fall as rows, V or K grow. */
+int rl_attn_token_logprobs(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale,
+                           rl_tensor* logprobs, rl_tensor* entropy, rl_tensor* lse, rl_tensor* top_ids,
+                           rl_tensor* top_logprobs, void* stream);
+size_t rl_attn_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int64_t top);
+
+/* The gradient of the logits: with g = d_logprobs[t], h = d_entropy[t],
+ *   d_logits_j = row_scale[t] (g (delta_j,token - p_j) - h p_j (ln p_j + entropy)).
+ *   logits, tokens, row_scale: as in the forward call; lse and entropy [T] f32 as it
+ *              wrote them (entropy is read only with d_entropy)
+ *   d_logprobs, d_entropy [T] f32, any stride from 0 on; one may be NULL (0)
+ *   d_logits   [T, V] of the logits' type, written; may be logits (the same view)
+ * Rows that are left out, or without a token above -inf, get zeros. */
+int rl_attn_token_logprobs_backward(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale,
+                                    const rl_tensor* lse, const rl_tensor* entropy, const rl_tensor* d_logprobs,
+                                    const rl_tensor* d_entropy, rl_tensor* d_logits, void* stream);
+
+/* ---- requests that begin and end, between steps ----
+ * rl_attn_map_slots takes pages from the list of free ones; these calls begin
+ * requests as copies of others and give pages back. */
+
+/* Requests that begin with tokens of others (paper: the G attempts of a group
+ * share their prompt, section "The Miles RL Loop"):
+ *   parents    [B] int32: request b takes over tokens of request parents[b];
+ *              negative: b is left as it is
+ *   fork_lens  [B] int32: how many, 0 <= n <= kv_lens[parents[b]]
+ *   kv_lens    [B] int32: tokens each request has; a forked one must have none, and
+ *              its parent must not be forked by the same call (reported, and b left
+ *              as it is, otherwise)
+ *   free_pages [F], free_used [1], page_size, num_pages: as for rl_attn_map_slots
+ *   block_table [B, max_pages] int32: the entries of b's ceil(n / P) pages are
+ *              written: the parent's n / P full pages, which they then share, and a
+ *              page of the list for the n mod P tokens behind
+ *   kv_lens_out [B], free_used_out [1] int32; may be kv_lens and free_used themselves
+ *   copies     [B, 3] int32: (page, own page, rows): the n mod P rows that
+ *              rl_attn_copy_pages has to copy in every layer; (-1, -1, 0) where there
+ *              are none
+ * Requests are served in order: from the first whose page the list does not have on,
+ * none is forked, which is reported. A page of the list that is outside the pool is
+ * reported, its request not forked. One launch (two for more than 4 requests in
+ * place). */
+int rl_attn_fork_requests(const rl_tensor* parents, const rl_tensor* fork_lens, const rl_tensor* kv_lens,
+                          const rl_tensor* free_pages, const rl_tensor* free_used, int64_t page_size,
+                          int64_t num_pages, rl_tensor* block_table, rl_tensor* kv_lens_out, rl_tensor* free_used_out,
+                          rl_tensor* copies, void* stream);
+
+/* Copies the first `rows` rows of pages to other pages, of K and of V:
+ *   copies     [n, 3] int32 (page, to page, rows), as rl_attn_fork_requests writes
+ *              them; rows <= 0: nothing to copy
+ *   k_pages, v_pages [num_pages, P, Hkv, 128] bf16 or E4M3 (the codes are copied: one
+ *              scale serves all pages of a head)
+ * A page outside the pool, or more rows than a page has, is reported and not
+ * copied. Pages that are copied to must differ from each other and from those
+ * copied from. */
+int rl_attn_copy_pages(const rl_tensor* copies, rl_tensor* k_pages, rl_tensor* v_pages, void* stream);
+
+/* Requests that end, or are cut back to an earlier token (a turn tried again,
+ * drafts that were refused):
+ *   kv_lens    [B] int32: tokens each request has
+ *   keep_lens  [B] int32: tokens it keeps: 0 ends it, kv_lens[b] or more leaves it
+ *              as it is (a negative one too, which is reported)
+ *   block_table [B, max_pages] int32, read: the requests' pages
+ *   free_pages [F] int32: pages that a request drops and that no request keeps are
+ *              written in front of the entries not taken, in the order of their ids
+ *   free_used  [1] int32
+ *   kv_lens_out [B], free_used_out [1] int32: min(kv_lens, keep_lens), and the entries
+ *              still taken; may be kv_lens and free_used themselves
+ * A page is kept as long as one request holds it within the tokens it keeps, so
+ * the tables say which pages are shared; a prefix kept for later requests is a request
+ * of its own. A request that is cut back inside a page it shares must be forked there
+ * before it grows (its next rows would be written to the others' page). Lengths past
+ * the table and page ids outside the pool are reported, and such pages not freed; if
+ * more pages come back than the list has lost, the ones with the highest ids are
+ * written and it is reported. Table entries are left as they are. */
+int rl_attn_drop_tokens(const rl_tensor* kv_lens, const rl_tensor* keep_lens, const rl_tensor* block_table,
+                        int64_t page_size, int64_t num_pages, rl_tensor* free_pages, const rl_tensor* free_used,
+                        rl_tensor* kv_lens_out, rl_tensor* free_used_out, void* stream);
+
 /* Causal attention over whole packed prompts (the first turn of a trajectory
  * group, before there is a cache to extend): row i of prompt b attends to its
  * rows 0 .. i, read from packed rows and not from pages.

@@ -18,7 +18,8 @@ LIB = os.path.join(PKG, "librlattn.so")
 PACK = os.path.join(PKG, "_pack.so")
 ARCH = os.environ.get("RL_ATTN_ARCH", "gfx950")
 
-SOURCES = ["decode.hip", "extend.hip", "append.hip", "map.hip", "rope.hip", "prefill.hip", "diag.hip", "scratch.hip", "rl_attn_host.cpp"]
+SOURCES = ["decode.hip", "extend.hip", "append.hip", "map.hip", "requests.hip", "rope.hip", "rope_grad.hip", "prefill.hip",
+           "logprob.hip", "diag.hip", "scratch.hip", "rl_attn_host.cpp"]
 
 
 def hipcc() -> str:

@@ -19,6 +19,9 @@ enum DeviceError : int {
   kErrPool = 128,    // the list of free pages is exhausted
   kErrSlot = 256,    // a slot at or past the end of the page pool
   kErrAxis = 512,    // an axis of a frequency outside the rows of positions (clamped)
+  kErrToken = 1024,  // a token at or past the end of the vocabulary
+  kErrRowScale = 2048,  // a scale of a row of logits that is not positive and finite
+  kErrParent = 4096, // a request that cannot be forked, or not into its place
 };
 
 // Slot markers of a decode piece: its result goes straight to out/lse, or
@@ -287,6 +290,106 @@ struct RopeArgs {
   int rows, Hq, Hkv, freqs, n_axes, interleaved, inverse;
   int parts;              // waves of a row
   int num_pages, page_size, log2_page;
+  // q and k rows are normed first: [128] weights, bf16 or fp32 (null: not normed)
+  const void* q_weight;
+  const void* k_weight;
+  int weights_f32;
+  float eps;
+  int* err;
+};
+
+// Gradient of normed and rotated rows. RopeArgs: q and k are the rows before, q_out and
+// k_out their gradients (written); Hkv = 0: no k.
+struct RopeGradArgs {
+  RopeArgs r;
+  const void* dq_out;     // gradients of the rows behind
+  const void* dk_out;
+  int64_t gq_st, gq_sh, gk_st, gk_sh;
+  float* dq_weight;       // [128], written
+  float* dk_weight;
+  int64_t dqw_s, dkw_s;
+  float* parts;           // [q_groups + k_groups, 128] workgroups' sums of the weights' gradients
+  int q_groups, k_groups; // workgroups of q and of k
+};
+constexpr int kRopeGradGroupsPerCu = 4;             // at most
+
+// Log probabilities of tokens, and the gradient of their logits.
+constexpr int kLogprobSegment = 4096;               // logits a wave sums at once
+constexpr int kLogprobChunks = 16;                  // workgroups of a row, at most
+constexpr int kLogprobTop = 32;                     // alternatives, at most
+constexpr int kLogprobPartBytes = 12;               // of a segment's sums
+struct LogprobArgs {
+  const void* x;          // [rows, vocab] bf16 or fp32
+  int64_t x_s;
+  const void* tokens;     // [rows] int32 or int64, negative: the row is left out
+  int64_t tok_s;
+  const float* scale;     // nullable: [rows]
+  int64_t scale_s;
+  float* logprobs;        // [rows]
+  float* entropy;         // nullable: [rows]
+  float* lse;             // nullable: [rows]
+  int64_t lp_s, ent_s, lse_s;
+  int* top_ids;           // [rows, top]
+  float* top_lps;
+  int64_t ti_s, tl_s;
+  // gradient (entropy and lse are read)
+  const float* d_lp;      // nullable: [rows]
+  const float* d_ent;     // nullable: [rows]
+  int64_t dlp_s, dent_s;
+  void* d_x;              // [rows, vocab], may be x
+  int64_t dx_s;
+  int rows, vocab, top, f32, tok64;
+  int chunks;             // workgroups of a row
+  int segs, segs_chunk;   // segments of a row and of a workgroup
+  void* parts;            // chunks > 1: [rows, segs] sums
+  uint64_t* cands;   // chunks > 1: [rows, chunks, top] ranked tokens
+  int* err;
+};
+
+// Requests that begin as copies of others.
+struct ForkArgs {
+  const int* parents;     // [B] request to fork from, negative: none
+  const int* fork_lens;   // [B] tokens taken over
+  const int* kv_lens;     // [B]
+  const int* free_pages;  // [n_free]
+  const int* free_used;
+  int64_t par_s, fl_s, kv_s, free_s;
+  int* bt;                // [B, max_pages]
+  int64_t bt_sb, bt_sj;
+  int* kv_out;            // [B] (may be kv_lens)
+  int* used_out;          // (may be free_used)
+  int* copies;            // [B, 3] source page, page, rows to be copied
+  int64_t kv_out_s, cp_s;
+  int B, n_free, num_pages, page_size, log2_page, max_pages;
+  int block;              // requests of a workgroup
+  int lengths, entries;   // what this launch writes: lengths and free entries, table entries and copies
+  int* err;
+};
+
+// Rows of pages to other pages.
+struct CopyArgs {
+  const int* copies;      // [n, 3]
+  int64_t cp_s;
+  char* k;
+  char* v;
+  int64_t kp_sp, kp_ss, kp_sh, vp_sp, vp_ss, vp_sh;   // bytes
+  int n, Hkv, row_bytes, num_pages, page_size;
+  int* err;
+};
+
+// Requests that end or are cut back.
+struct DropArgs {
+  const int* kv_lens;     // [B]
+  const int* keep_lens;   // [B]
+  const int* bt;
+  int64_t kv_s, keep_s, bt_sb, bt_sj;
+  int* free_pages;        // [n_free], written in front of *free_used
+  const int* free_used;
+  int64_t free_s;
+  int* kv_out;            // [B] (may be kv_lens)
+  int* used_out;          // (may be free_used)
+  int64_t kv_out_s;
+  int B, n_free, num_pages, page_size, log2_page, max_pages;
   int* err;
 };
 
@@ -349,6 +452,13 @@ hipError_t launch_merge(const MergeArgs& a, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream, KernelTimer* timer);
 hipError_t launch_map(const MapArgs& a, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs& args, int cus, hipStream_t stream, KernelTimer* timer);
+hipError_t launch_rope_grad(const RopeGradArgs& args, hipStream_t stream, KernelTimer* timer);
+int logprob_chunks(int64_t rows, int vocab, int cus);
+hipError_t launch_logprob(const LogprobArgs& args, hipStream_t stream);
+hipError_t launch_logprob_grad(const LogprobArgs& args, hipStream_t stream);
+hipError_t launch_fork(const ForkArgs& args, hipStream_t stream);
+hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream);
+hipError_t launch_drop(const DropArgs& a, hipStream_t stream);
 hipError_t launch_prefill(const PrefillArgs& a, int cus, hipStream_t stream, KernelTimer* timer);
 
 }  // namespace rl

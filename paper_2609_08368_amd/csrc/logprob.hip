@@ -1,0 +1,477 @@
+// Log probabilities of given tokens, with the entropy of their distribution and
+// its likeliest tokens, from a step's logits; and the gradient of the logits.
+//
+// With z_j = s x_j (s the row's scale), lse = ln sum_j exp z_j:
+//   logprob = z_token - lse,   entropy = lse - sum_j p_j z_j,   p_j = exp(z_j - lse).
+// A row is cut into segments of kSegment logits. A wave holds a whole segment in
+// registers: it takes the segment's maximum m first, then S = sum_j 2^y_j and
+// Y = sum_j 2^y_j y_j with y_j = (x_j - m) s log2 e, so nothing is rescaled on the
+// way. The segments' (m, S, Y) are folded in one fixed tree whatever workgroup
+// made them, so that a row's bits depend on its logits alone: not on the size of
+// the call, on how its rows are shared out or on where they lie.
+//   lse = s M + ln 2 log2 S,  entropy = ln 2 (log2 S - Y / S)
+// (all terms of one size, none cancelled: Y is taken around the maximum).
+//
+// Alternatives: the K-th largest of a workgroup's threads' maxima is a lower
+// bound of the K-th largest logit, so only the threads whose maximum reaches it
+// hold any of the K likeliest; their logits, about K / 256 of all, are read
+// again, and the few that reach the bound are ranked.
+//
+// A call is one pass over the logits, HBM-bound.
+#include <algorithm>
+
+#include "attn_common.hpp"
+#include "kernels.hpp"
+
+namespace rl {
+
+namespace {
+
+constexpr int kLpThreads = 256, kLpWaves = kLpThreads / 64;
+constexpr int kSegment = kLogprobSegment;
+constexpr int kCand = 512;                          // candidates that are ranked at once
+constexpr uint32_t kKeyNegInf = 0x007fffffu;        // key_of(-inf)
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+// (rows may start at any element: a vocabulary need not be a multiple of 16 bytes)
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+// Logits of type X in sixteen bytes, and those as fp32.
+template <typename X>
+constexpr int kPer = 16 / (int)sizeof(X);
+template <typename X>
+__device__ __forceinline__ void unpack(u32x4 w, float (&f)[kPer<X>]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(X) == 2) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+      f[i] = __uint_as_float(w[i]);
+    }
+  }
+}
+template <typename X>
+__device__ __forceinline__ u32x4 pack(const float (&f)[kPer<X>]) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(X) == 2)
+      w[i] = __builtin_bit_cast(u16, (__bf16)f[2 * i]) | (uint32_t)__builtin_bit_cast(u16, (__bf16)f[2 * i + 1]) << 16;
+    else
+      w[i] = __float_as_uint(f[i]);
+  }
+  return w;
+}
+// Sixteen bytes of logits from element e of n on; those behind the end are -inf.
+template <typename X>
+__device__ __forceinline__ u32x4 load_logits(const X* x, int e, int n) {
+  if (e + kPer<X> <= n) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(x + e));
+  float f[kPer<X>];
+#pragma unroll
+  for (int i = 0; i < kPer<X>; ++i) f[i] = e + i < n ? (float)x[e + i] : kNegInf;
+  return pack<X>(f);
+}
+
+// An order of floats as whole numbers: NaN lowest, both zeros one.
+__device__ __forceinline__ uint32_t key_of(float f) {
+  uint32_t u = __float_as_uint(f);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
+  if (u == 0x80000000u) u = 0;
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float float_of(uint32_t key) {
+  return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
+}
+// The larger logit first, of equal ones the lower index. Never 0.
+__device__ __forceinline__ uint64_t rank_of(uint32_t key, int index) {
+  return (uint64_t)key << 32 | (0xffffffffu - (uint32_t)index);
+}
+
+// A row's token and scale; token < 0: the row is left out.
+struct RowInput {
+  int token;
+  float scale;
+};
+__device__ __forceinline__ RowInput read_row(const LogprobArgs& a, int64_t r, int* bad) {
+  const int64_t t = a.tok64 ? static_cast<const int64_t*>(a.tokens)[r * a.tok_s]
+                            : (int64_t)static_cast<const int*>(a.tokens)[r * a.tok_s];
+  RowInput in{t < 0 ? -1 : (int)min(t, (int64_t)a.vocab), a.scale ? a.scale[r * a.scale_s] : 1.f};
+  if (in.token == a.vocab) {
+    *bad |= kErrToken;
+    in.token = -1;
+  }
+  if (!scale_ok(in.scale)) {
+    if (t >= 0) *bad |= kErrRowScale;
+    in.token = -1;
+  }
+  return in;
+}
+
+// One segment's maximum and sums.
+struct Part {
+  float m, s, y;
+};
+
+// A wave's segment of n logits at x; *lane_max is the largest of this lane's.
+template <typename X>
+__device__ __forceinline__ Part segment_part(const X* x, int n, float c, float* lane_max) {
+  constexpr int kLoads = kSegment / 64 / kPer<X>;
+  const int at = (threadIdx.x & 63) * kPer<X>;
+  u32x4 w[kLoads];
+  if (n == kSegment) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(x + at + i * 64 * kPer<X>));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) w[i] = load_logits(x, at + i * 64 * kPer<X>, n);
+  }
+  float top = kNegInf;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    float f[kPer<X>];
+    unpack<X>(w[i], f);
+#pragma unroll
+    for (int e = 0; e < kPer<X>; ++e) top = fmaxf(top, f[e]);
+  }
+  *lane_max = top;
+  Part p{wave_max(top), 0.f, 0.f};
+  const float m = p.m == kNegInf ? 0.f : p.m;       // (excluded tokens alone: every term is 0)
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    float f[kPer<X>];
+    unpack<X>(w[i], f);
+#pragma unroll
+    for (int e = 0; e < kPer<X>; ++e) {
+      const float y = (f[e] - m) * c, t = exp2_fast(y);
+      p.s += t;
+      p.y = fmaf(t, fmaxf(y, -1000.f), p.y);        // (0 times -inf)
+    }
+  }
+  p.s = wave_sum(p.s);
+  p.y = wave_sum(p.y);
+  return p;
+}
+
+// The row's sums from its segments' (a wave; every lane receives them).
+__device__ __forceinline__ Part fold_parts(const Part* parts, int n, float c) {
+  const int lane = threadIdx.x & 63;
+  float m = kNegInf;
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, parts[i].m);
+  Part row{wave_max(m), 0.f, 0.f};
+  for (int i = lane; i < n; i += 64) {
+    const Part p = parts[i];
+    const float d = p.m == kNegInf ? 0.f : fmaxf((p.m - row.m) * c, -1000.f), f = exp2_fast(d);
+    row.s = fmaf(f, p.s, row.s);
+    row.y = fmaf(f, fmaf(d, p.s, p.y), row.y);
+  }
+  row.s = wave_sum(row.s);
+  row.y = wave_sum(row.y);
+  return row;
+}
+
+// What a row answers with, from its sums.
+struct RowStats {
+  float m, log2s;
+  bool none;                                        // every token is excluded
+};
+__device__ __forceinline__ float log_prob(const RowStats& r, float x, float scale) {
+  return r.none ? kNegInf : (x - r.m) * scale - kLn2 * r.log2s;
+}
+
+template <typename X>
+__device__ __forceinline__ RowStats write_row(const LogprobArgs& a, int64_t r, const RowInput& in, const Part& p) {
+  // (bits, not comparisons: the device code is compiled as if there were no NaN)
+  const RowStats st{p.m, __builtin_amdgcn_logf(p.s), (__float_as_uint(p.s) << 1) == 0};
+  if ((threadIdx.x & 63) == 0) {
+    const float x = (float)(static_cast<const X*>(a.x)[r * a.x_s + in.token]);
+    a.logprobs[r * a.lp_s] = log_prob(st, x, in.scale);
+    if (a.lse) a.lse[r * a.lse_s] = st.none ? kNegInf : fmaf(p.m, in.scale, kLn2 * st.log2s);
+    if (a.entropy) {
+      float h = kLn2 * (st.log2s - p.y / p.s);
+      const uint32_t u = __float_as_uint(h);
+      if (st.none || (u >= 0x80000000u && u <= 0xff800000u)) h = 0.f;     // (a rounding below 0)
+      a.entropy[r * a.ent_s] = h;
+    }
+  }
+  return st;
+}
+
+// A row without a token.
+__device__ __forceinline__ void write_masked(const LogprobArgs& a, int64_t r) {
+  const int tid = threadIdx.x;
+  if (tid == 0) {
+    a.logprobs[r * a.lp_s] = 0.f;
+    if (a.lse) a.lse[r * a.lse_s] = 0.f;
+    if (a.entropy) a.entropy[r * a.ent_s] = 0.f;
+  }
+  if (tid < a.top) {
+    a.top_ids[r * a.ti_s + tid] = -1;
+    a.top_lps[r * a.tl_s + tid] = kNegInf;
+  }
+}
+
+struct TopLds {
+  uint32_t keys[kLpThreads];
+  uint64_t cand[kCand];
+  uint64_t best[kLogprobTop];
+  uint32_t tau;
+  int winners[kLpThreads];
+  int n_winners, n_cand;
+};
+
+// The `top` largest of t.cand[0 .. n) to t.best, in order; 0 behind the last.
+__device__ __forceinline__ void rank_candidates(TopLds& t, int n, int top) {
+  const int tid = threadIdx.x;
+  if (tid < top) t.best[tid] = 0;
+  __syncthreads();
+  for (int i = tid; i < n; i += kLpThreads) {
+    const uint64_t mine = t.cand[i];
+    int rank = 0;
+    for (int j = 0; j < n && rank < top; ++j) rank += t.cand[j] > mine;
+    if (mine != 0 && rank < top) t.best[rank] = mine;
+  }
+  __syncthreads();
+}
+
+// The workgroup's likeliest tokens to t.best: of segments seg0 .. seg1-1 of row x,
+// where wave w has seg0 + w, seg0 + w + kLpWaves, ... and lane_max is this
+// thread's largest logit of those.
+template <typename X>
+__device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int seg0, int seg1, float lane_max, int top) {
+  constexpr int kLoads = kSegment / 64 / kPer<X>;
+  const int tid = threadIdx.x;
+  const uint32_t key = key_of(lane_max);
+  t.keys[tid] = key;
+  if (tid == 0) t.n_winners = t.n_cand = 0;
+  __syncthreads();
+  int rank = 0;
+#pragma unroll 4
+  for (int j = 0; j < kLpThreads; ++j) rank += t.keys[j] > key || (t.keys[j] == key && j < tid);
+  if (rank == top - 1) t.tau = key;
+  __syncthreads();
+  const uint32_t tau = max(t.tau, kKeyNegInf + 1);  // excluded tokens are no alternatives
+  if (key >= tau) t.winners[atomicAdd(&t.n_winners, 1)] = tid;
+  __syncthreads();
+  const int rounds = (seg1 - seg0 + kLpWaves - 1) / kLpWaves, per = rounds * kLoads, n = t.n_winners * per;
+  for (int p = tid; p < n; p += kLpThreads) {
+    const int who = t.winners[p / per], i = p % per;
+    const int seg = seg0 + (who >> 6) + (i / kLoads) * kLpWaves;
+    const int e = seg * kSegment + ((i % kLoads) * 64 + (who & 63)) * kPer<X>;
+    if (seg >= seg1 || e >= vocab) continue;
+    float f[kPer<X>];
+    unpack<X>(load_logits(x, e, vocab), f);
+#pragma unroll
+    for (int j = 0; j < kPer<X>; ++j) {
+      const uint32_t k = key_of(f[j]);
+      if (k < tau) continue;
+      const int at = atomicAdd(&t.n_cand, 1);
+      if (at < kCand) t.cand[at] = rank_of(k, e + j);
+    }
+  }
+  __syncthreads();
+  int found = t.n_cand;
+  if (found > kCand) {
+    // so many equal logits that the list does not hold them: one after the other,
+    // each the largest below the last
+    const int lo = seg0 * kSegment, hi = min(vocab, seg1 * kSegment);
+    uint64_t below = ~0ull;
+    for (found = 0; found < top; ++found) {
+      uint64_t most = 0;
+      for (int e = lo + tid; e < hi; e += kLpThreads) {
+        const uint64_t v = rank_of(key_of((float)x[e]), e);
+        if (v < below && v > most) most = v;
+      }
+      __syncthreads();                              // (the last round's list has been read)
+      t.cand[tid] = most;
+      __syncthreads();
+      for (int s = kLpThreads / 2; s > 0; s >>= 1) {
+        if (tid < s && t.cand[tid + s] > t.cand[tid]) t.cand[tid] = t.cand[tid + s];
+        __syncthreads();
+      }
+      below = t.cand[0];
+      if ((uint32_t)(below >> 32) <= kKeyNegInf) break;
+      if (tid == 0) t.best[found] = below;
+    }
+    if (tid < top && tid >= found) t.best[tid] = 0;
+    __syncthreads();
+    return;
+  }
+  rank_candidates(t, found, top);
+}
+
+// t.best as the row's alternatives.
+__device__ __forceinline__ void write_top(const LogprobArgs& a, int64_t r, const TopLds& t, const RowStats& st,
+                                          float scale) {
+  const int i = threadIdx.x;
+  if (i >= a.top) return;
+  const uint64_t b = t.best[i];
+  a.top_ids[r * a.ti_s + i] = b ? (int)(0xffffffffu - (uint32_t)b) : -1;
+  a.top_lps[r * a.tl_s + i] = b ? log_prob(st, float_of((uint32_t)(b >> 32)), scale) : kNegInf;
+}
+
+// Workgroup: segments of one row. Where a row is one workgroup's, that answers;
+// otherwise the segments' sums and the workgroup's likeliest tokens go to memory.
+template <typename X, bool kTop>
+__global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobArgs a) {
+  extern __shared__ Part parts[];                   // [segs_chunk]
+  __shared__ TopLds top;
+  const int row32 = blockIdx.x / a.chunks, chunk = blockIdx.x - row32 * a.chunks;
+  const int64_t r = row32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int bad = 0;
+  const RowInput in = read_row(a, r, &bad);
+  if (in.token < 0) {
+    if (chunk != 0) return;
+    if (bad && threadIdx.x == 0) atomicOr(a.err, bad);
+    write_masked(a, r);
+    return;
+  }
+  const X* x = static_cast<const X*>(a.x) + r * a.x_s;
+  const float c = in.scale * kLog2e;
+  const int seg0 = chunk * a.segs_chunk, seg1 = min(a.segs, seg0 + a.segs_chunk);
+  float most = kNegInf;
+  for (int s = seg0 + wave; s < seg1; s += kLpWaves) {
+    float lane_max;
+    const Part p = segment_part(x + s * kSegment, min(kSegment, a.vocab - s * kSegment), c, &lane_max);
+    most = fmaxf(most, lane_max);
+    if ((threadIdx.x & 63) == 0) {
+      if (a.chunks == 1)
+        parts[s] = p;
+      else
+        reinterpret_cast<Part*>(a.parts)[r * a.segs + s] = p;
+    }
+  }
+  if constexpr (kTop) find_top(top, x, a.vocab, seg0, seg1, most, a.top);
+  if (a.chunks > 1) {
+    if (kTop && threadIdx.x < a.top) a.cands[(r * a.chunks + chunk) * a.top + threadIdx.x] = top.best[threadIdx.x];
+    return;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const RowStats st = write_row<X>(a, r, in, fold_parts(parts, a.segs, c));
+    if (kTop) write_top(a, r, top, st, in.scale);
+  }
+}
+
+// Workgroup: one row of several workgroups' parts.
+template <typename X, bool kTop>
+__global__ __launch_bounds__(kLpThreads) void logprob_join_kernel(LogprobArgs a) {
+  __shared__ TopLds top;
+  const int64_t r = blockIdx.x;
+  int bad = 0;
+  const RowInput in = read_row(a, r, &bad);
+  if (in.token < 0) return;                         // (written and reported by its first workgroup)
+  if constexpr (kTop) {
+    const int n = a.chunks * a.top;
+    for (int i = threadIdx.x; i < n; i += kLpThreads) top.cand[i] = a.cands[r * n + i];
+    __syncthreads();
+    rank_candidates(top, n, a.top);
+  }
+  if (threadIdx.x >= 64) return;
+  const Part p = fold_parts(reinterpret_cast<const Part*>(a.parts) + r * a.segs, a.segs, in.scale * kLog2e);
+  const RowStats st = write_row<X>(a, r, in, p);
+  if (kTop) write_top(a, r, top, st, in.scale);
+}
+
+// Gradient: d_x_j = s (g (delta_j - p_j) - h p_j (ln p_j + H)), an element-wise pass.
+constexpr int kGradLoads = 4;
+
+template <typename X>
+__global__ __launch_bounds__(kLpThreads) void logprob_grad_kernel(LogprobArgs a) {
+  const int row32 = blockIdx.x / a.chunks, chunk = blockIdx.x - row32 * a.chunks;
+  const int64_t r = row32;
+  int bad = 0;
+  const RowInput in = read_row(a, r, &bad);
+  if (bad && chunk == 0 && threadIdx.x == 0) atomicOr(a.err, bad);
+  const X* x = static_cast<const X*>(a.x) + r * a.x_s;
+  X* d = static_cast<X*>(a.d_x) + r * a.dx_s;
+  const int e0 = (chunk * kGradLoads * kLpThreads + threadIdx.x) * kPer<X>;
+  float lse = 0.f, g = 0.f, h = 0.f, ent = 0.f;
+  if (in.token >= 0) {
+    lse = a.lse[r * a.lse_s];
+    if (a.d_lp) g = a.d_lp[r * a.dlp_s];
+    if (a.d_ent) {
+      h = a.d_ent[r * a.dent_s];
+      ent = a.entropy[r * a.ent_s];
+    }
+  }
+  if (in.token < 0 || lse == kNegInf) {             // left out, or every token excluded
+#pragma unroll
+    for (int i = 0; i < kGradLoads; ++i) {
+      const int e = e0 + i * kLpThreads * kPer<X>;
+      if (e + kPer<X> <= a.vocab)
+        __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4_any*>(d + e));
+      else
+        for (int j = e; j < a.vocab; ++j) d[j] = (X)0.f;
+    }
+    return;
+  }
+  u32x4 w[kGradLoads];
+#pragma unroll
+  for (int i = 0; i < kGradLoads; ++i) w[i] = load_logits(x, e0 + i * kLpThreads * kPer<X>, a.vocab);
+#pragma unroll
+  for (int i = 0; i < kGradLoads; ++i) {
+    const int e = e0 + i * kLpThreads * kPer<X>;
+    float f[kPer<X>];
+    unpack<X>(w[i], f);
+#pragma unroll
+    for (int j = 0; j < kPer<X>; ++j) {
+      const float lp = fmaf(f[j], in.scale, -lse), p = exp2_fast(lp * kLog2e);
+      const float v = -p * fmaf(h, fmaxf(lp, -1000.f) + ent, g);          // (0 times -inf)
+      f[j] = in.scale * (e + j == in.token ? v + g : v);
+    }
+    if (e + kPer<X> <= a.vocab)
+      __builtin_nontemporal_store(pack<X>(f), reinterpret_cast<u32x4_any*>(d + e));
+    else
+#pragma unroll
+      for (int j = 0; j < kPer<X>; ++j)
+        if (e + j < a.vocab) d[e + j] = (X)f[j];
+  }
+}
+
+}  // namespace
+
+// Workgroups of a row: one where the rows fill the device, else as many as that
+// takes, of four segments at least.
+int logprob_chunks(int64_t rows, int vocab, int cus) {
+  const int segs = (vocab + kSegment - 1) / kSegment;
+  const int64_t want = std::max<int64_t>(1, (8 * (int64_t)cus + rows - 1) / std::max<int64_t>(rows, 1));
+  const int most = std::min(kLogprobChunks, (segs + kLpWaves - 1) / kLpWaves);
+  const int chunks = (int)std::min<int64_t>(want, std::max(1, most));
+  const int each = ((segs + chunks - 1) / chunks + kLpWaves - 1) / kLpWaves * kLpWaves;
+  return std::max(1, (segs + each - 1) / each);
+}
+
+hipError_t launch_logprob(const LogprobArgs& args, hipStream_t stream) {
+  LogprobArgs a = args;
+  a.segs = (a.vocab + kSegment - 1) / kSegment;
+  a.segs_chunk = ((a.segs + a.chunks - 1) / a.chunks + kLpWaves - 1) / kLpWaves * kLpWaves;
+  const unsigned grid = (unsigned)((int64_t)a.rows * a.chunks);
+  const size_t lds = a.chunks == 1 ? sizeof(Part) * (size_t)a.segs : 0;
+  auto run = [&](auto type, auto top) {
+    typedef decltype(type) X;
+    logprob_kernel<X, decltype(top)::value><<<grid, kLpThreads, lds, stream>>>(a);
+    if (a.chunks > 1) logprob_join_kernel<X, decltype(top)::value><<<(unsigned)a.rows, kLpThreads, 0, stream>>>(a);
+  };
+  if (a.f32)
+    a.top ? run(float{}, std::true_type{}) : run(float{}, std::false_type{});
+  else
+    a.top ? run(__bf16{}, std::true_type{}) : run(__bf16{}, std::false_type{});
+  return hipGetLastError();
+}
+
+hipError_t launch_logprob_grad(const LogprobArgs& args, hipStream_t stream) {
+  LogprobArgs a = args;
+  const int64_t each = (int64_t)kGradLoads * kLpThreads * (a.f32 ? kPer<float> : kPer<__bf16>);
+  a.chunks = (int)((a.vocab + each - 1) / each);
+  const unsigned grid = (unsigned)((int64_t)a.rows * a.chunks);
+  if (a.f32)
+    logprob_grad_kernel<float><<<grid, kLpThreads, 0, stream>>>(a);
+  else
+    logprob_grad_kernel<__bf16><<<grid, kLpThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace rl

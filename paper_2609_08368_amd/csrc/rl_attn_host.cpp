@@ -1227,21 +1227,86 @@ int fill_slots(const rl_tensor* k, const rl_tensor* v, int kv_dtype, const rl_te
   return RL_OK;
 }
 
-int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const rl_tensor* positions,
+// Weights and eps of the norms of q and k rows (k_weight NULL: there is no k).
+struct Norm {
+  const rl_tensor *q_weight, *k_weight;
+  float eps;
+};
+int check_weight(const rl_tensor* t, const char* name, int dtype) {
+  RL_TRY(check_view(t, name, 1));
+  if (t->dtype != RL_BF16 && t->dtype != RL_F32) return fail(RL_ERR_DTYPE, "%s must be bf16 or f32", name);
+  if (t->dtype != dtype) return fail(RL_ERR_DTYPE, "q_weight and k_weight must have one type");
+  if (t->shape[0] != 128) return fail(RL_ERR_SHAPE, "%s must have 128 entries (got %lld)", name, (long long)t->shape[0]);
+  if (t->strides[0] != 1) return fail(RL_ERR_UNSUPPORTED, "%s: stride must be 1", name);
+  if (reinterpret_cast<uintptr_t>(t->data) % 16 != 0)
+    return fail(RL_ERR_UNSUPPORTED, "%s: data must be 16-byte aligned", name);
+  return check_data(t, name);
+}
+int fill_norm(const Norm& n, bool has_k, rl::RopeArgs* a) {
+  RL_TRY(check_view(n.q_weight, "q_weight", 1));
+  RL_TRY(check_weight(n.q_weight, "q_weight", n.q_weight->dtype));
+  if (has_k) RL_TRY(check_weight(n.k_weight, "k_weight", n.q_weight->dtype));
+  if (!has_k && n.k_weight) return fail(RL_ERR_INVALID_ARG, "k_weight is given, but k is NULL");
+  // (a subnormal eps may be taken as zero, and then a row of zeros as NaN)
+  if (!(n.eps >= 1.17549435e-38f) || !std::isfinite(n.eps))
+    return fail(RL_ERR_INVALID_ARG, "eps must be positive and finite (got %g)", (double)n.eps);
+  a->q_weight = n.q_weight->data;
+  a->k_weight = has_k ? n.k_weight->data : nullptr;
+  a->weights_f32 = n.q_weight->dtype == RL_F32;
+  a->eps = n.eps;
+  return RL_OK;
+}
+
+// Options of a rotary call (why: the calls that `inverse` is for, NULL if it may be given).
+int fill_rope_opts(const rl_rope_opts* opts, const char* why, rl::RopeArgs* a) {
+  if (!opts) return RL_OK;
+  for (int i = 0; i < 6; ++i)
+    if (opts->reserved[i] != 0) return fail(RL_ERR_INVALID_ARG, "opts.reserved[%d] must be zero", i);
+  if (opts->interleaved != 0 && opts->interleaved != 1)
+    return fail(RL_ERR_INVALID_ARG, "opts.interleaved must be 0 or 1");
+  if (opts->inverse != 0 && opts->inverse != 1) return fail(RL_ERR_INVALID_ARG, "opts.inverse must be 0 or 1");
+  if (opts->inverse && why) return fail(RL_ERR_INVALID_ARG, "opts.inverse is for %s", why);
+  a->interleaved = opts->interleaved;
+  a->inverse = opts->inverse;
+  return RL_OK;
+}
+
+// Positions, frequencies and axes of a rotary call.
+int fill_turns(const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes, int64_t rows,
+               rl::RopeArgs* a) {
+  RL_TRY(check_view(inv_freq, "inv_freq", 1));
+  const int64_t F = inv_freq->shape[0];
+  RL_TRY(check_vector(inv_freq, "inv_freq", RL_F32, F, false));
+  if (F < 8 || F > 64 || F % 8 != 0)
+    return fail(RL_ERR_UNSUPPORTED, "inv_freq must have a multiple of 8 entries, 8 to 64 (got %lld)", (long long)F);
+  RL_TRY(check_view(positions, "positions", 2));
+  RL_TRY(check_dtype(positions, "positions", RL_I32));
+  if (positions->shape[0] < 1 || positions->shape[0] > 64 || positions->shape[1] != rows)
+    return fail(RL_ERR_SHAPE, "positions must be [axes, rows] with 1 to 64 axes");
+  if (positions->strides[0] < 0 || positions->strides[1] < 0)
+    return fail(RL_ERR_UNSUPPORTED, "positions: strides must be non-negative");
+  RL_TRY(check_data(positions, "positions"));
+  if (axes) RL_TRY(check_vector(axes, "axes", RL_I32, F, false));
+  if (!axes && positions->shape[0] != 1)
+    return fail(RL_ERR_INVALID_ARG, "axes is NULL, but positions has %lld axes", (long long)positions->shape[0]);
+  a->pos = static_cast<const int*>(positions->data);
+  a->pos_sa = positions->strides[0];
+  a->pos_st = positions->strides[1];
+  a->inv_freq = static_cast<const float*>(inv_freq->data);
+  a->freq_s = inv_freq->strides[0];
+  a->axes = axes ? static_cast<const int*>(axes->data) : nullptr;
+  a->axes_s = axes ? axes->strides[0] : 0;
+  a->freqs = (int)F;
+  a->n_axes = (int)positions->shape[0];
+  return RL_OK;
+}
+
+int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const Norm* norm, const rl_tensor* positions,
               const rl_tensor* inv_freq, const rl_tensor* axes, const rl_rope_opts* opts, const rl_tensor* slot_map,
               rl_tensor* q_out, rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, bool append, int kv_dtype,
               const rl_tensor* k_scale, const rl_tensor* v_scale, void* stream) {
   rl::RopeArgs a{};
-  if (opts) {
-    for (int i = 0; i < 6; ++i)
-      if (opts->reserved[i] != 0) return fail(RL_ERR_INVALID_ARG, "opts.reserved[%d] must be zero", i);
-    if (opts->interleaved != 0 && opts->interleaved != 1)
-      return fail(RL_ERR_INVALID_ARG, "opts.interleaved must be 0 or 1");
-    if (opts->inverse != 0 && opts->inverse != 1) return fail(RL_ERR_INVALID_ARG, "opts.inverse must be 0 or 1");
-    if (opts->inverse && append) return fail(RL_ERR_INVALID_ARG, "opts.inverse is for rows that are not appended");
-    a.interleaved = opts->interleaved;
-    a.inverse = opts->inverse;
-  }
+  RL_TRY(fill_rope_opts(opts, append ? "rows that are not appended" : norm ? "rows that are not normed" : nullptr, &a));
   const char* k_name = append ? "k_new" : "k";
   RL_TRY(check_view(q, "q", 3));
   const int64_t rows = q->shape[0], Hq = q->shape[1];
@@ -1261,21 +1326,8 @@ int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const 
   if (rows > (1 << 25) || Hq > 4096 || Hkv > 4096)
     return fail(RL_ERR_UNSUPPORTED, "rows or head count too large");
   if (rows * ((Hq + 2 * Hkv + 15) / 16) >= (1 << 26)) return fail(RL_ERR_UNSUPPORTED, "rows times heads too large");
-  RL_TRY(check_view(inv_freq, "inv_freq", 1));
-  const int64_t F = inv_freq->shape[0];
-  RL_TRY(check_vector(inv_freq, "inv_freq", RL_F32, F, false));
-  if (F < 8 || F > 64 || F % 8 != 0)
-    return fail(RL_ERR_UNSUPPORTED, "inv_freq must have a multiple of 8 entries, 8 to 64 (got %lld)", (long long)F);
-  RL_TRY(check_view(positions, "positions", 2));
-  RL_TRY(check_dtype(positions, "positions", RL_I32));
-  if (positions->shape[0] < 1 || positions->shape[0] > 64 || positions->shape[1] != rows)
-    return fail(RL_ERR_SHAPE, "positions must be [axes, rows] with 1 to 64 axes");
-  if (positions->strides[0] < 0 || positions->strides[1] < 0)
-    return fail(RL_ERR_UNSUPPORTED, "positions: strides must be non-negative");
-  RL_TRY(check_data(positions, "positions"));
-  if (axes) RL_TRY(check_vector(axes, "axes", RL_I32, F, false));
-  if (!axes && positions->shape[0] != 1)
-    return fail(RL_ERR_INVALID_ARG, "axes is NULL, but positions has %lld axes", (long long)positions->shape[0]);
+  RL_TRY(fill_turns(positions, inv_freq, axes, rows, &a));
+  if (norm) RL_TRY(fill_norm(*norm, k != nullptr, &a));
   if (append) {
     RL_TRY(check_vector(slot_map, "slot_map", RL_I64, rows, false));
     RL_TRY(fill_slots(k_pages, v_pages, kv_dtype, k_scale, v_scale, Hkv, &a));
@@ -1286,9 +1338,10 @@ int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const 
     a.v_sh = v->strides[1];
   }
   if (rows == 0 || Hq + Hkv == 0) return RL_OK;
-  const Named outs[] = {{q_out, "q_out"}, {k_out, "k_out"}}, ins[] = {{q, "q"}, {k, k_name}, {v, "v_new"}};
+  const Named outs[] = {{q_out, "q_out"}, {k_out, "k_out"}}, ins[] = {{q, "q"}, {k, k_name}, {v, "v_new"},
+                        {norm ? norm->q_weight : nullptr, "q_weight"}, {norm ? norm->k_weight : nullptr, "k_weight"}};
   const rl_tensor* same[] = {q, k};
-  RL_TRY(check_apart(outs, same, 2, ins, 3));
+  RL_TRY(check_apart(outs, same, 2, ins, 5));
   int cus = 0;
   RL_TRY(current_cus(&cus));
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -1310,24 +1363,463 @@ int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const 
     a.ko_st = k_out->strides[0];
     a.ko_sh = k_out->strides[1];
   }
-  a.pos = static_cast<const int*>(positions->data);
-  a.pos_sa = positions->strides[0];
-  a.pos_st = positions->strides[1];
-  a.inv_freq = static_cast<const float*>(inv_freq->data);
-  a.freq_s = inv_freq->strides[0];
-  a.axes = axes ? static_cast<const int*>(axes->data) : nullptr;
-  a.axes_s = axes ? axes->strides[0] : 0;
   a.rows = (int)rows;
   a.Hq = (int)Hq;
   a.Hkv = (int)Hkv;
-  a.freqs = (int)F;
-  a.n_axes = (int)positions->shape[0];
   a.err = w->err;
   rl::KernelTimer slot;
   rl::KernelTimer* timer = prof_timer(&slot, st);
   const hipError_t e = rl::launch_rope(a, cus, st, timer);
   prof_commit(4, timer);
   if (e != hipSuccess) return hip_fail(e, "rotary kernel launch");
+  return RL_OK;
+}
+
+// Workgroups of q rows and of k rows of a gradient call: what the device holds at once, shared in proportion, a wave
+// with at least one unit of eight head rows.
+void rope_grad_groups(int64_t rows, int64_t Hq, int64_t Hkv, int cus, int* q_groups, int* k_groups) {
+  const int64_t uq = rows * ((Hq + 7) / 8), uk = rows * ((Hkv + 7) / 8), all = (int64_t)rl::kRopeGradGroupsPerCu * cus;
+  auto share = [&](int64_t u) {
+    if (u == 0) return (int64_t)0;
+    const int64_t most = (u + 3) / 4;
+    return std::min(most, std::max<int64_t>(1, (all * u + uq + uk - 1) / (uq + uk)));
+  };
+  *q_groups = (int)share(uq);
+  *k_groups = (int)share(uk);
+}
+
+size_t rope_grad_bytes(int cus) { return ((size_t)rl::kRopeGradGroupsPerCu * cus + 2) * 128 * sizeof(float); }
+
+int rope_grad_impl(const rl_tensor* dq_out, const rl_tensor* dk_out, const rl_tensor* q, const rl_tensor* k,
+                   const Norm& norm, const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                   const rl_rope_opts* opts, rl_tensor* dq, rl_tensor* dk, rl_tensor* dq_weight, rl_tensor* dk_weight,
+                   void* stream) {
+  rl::RopeGradArgs g{};
+  rl::RopeArgs& a = g.r;
+  RL_TRY(fill_rope_opts(opts, "rows that are not normed", &a));
+  RL_TRY(check_view(q, "q", 3));
+  const int64_t rows = q->shape[0], Hq = q->shape[1];
+  RL_TRY(check_head_rows(q, "q", rows, Hq, false));
+  RL_TRY(check_head_rows(dq_out, "dq_out", rows, Hq, false));
+  RL_TRY(check_head_rows(dq, "dq", rows, Hq, true));
+  RL_TRY(check_vector(dq_weight, "dq_weight", RL_F32, 128, true));
+  int64_t Hkv = 0;
+  if (k) {
+    RL_TRY(check_view(k, "k", 3));
+    Hkv = k->shape[1];
+    RL_TRY(check_head_rows(k, "k", rows, Hkv, false));
+    RL_TRY(check_head_rows(dk_out, "dk_out", rows, Hkv, false));
+    RL_TRY(check_head_rows(dk, "dk", rows, Hkv, true));
+    RL_TRY(check_vector(dk_weight, "dk_weight", RL_F32, 128, true));
+  } else if (dk_out || dk || dk_weight) {
+    return fail(RL_ERR_INVALID_ARG, "k is NULL");
+  }
+  if (rows > (1 << 25) || Hq > 4096 || Hkv > 4096)
+    return fail(RL_ERR_UNSUPPORTED, "rows or head count too large");
+  if (rows * ((Hq + 2 * Hkv + 15) / 16) >= (1 << 26)) return fail(RL_ERR_UNSUPPORTED, "rows times heads too large");
+  RL_TRY(fill_turns(positions, inv_freq, axes, rows, &a));
+  RL_TRY(fill_norm(norm, k != nullptr, &a));
+  const Named outs[] = {{dq, "dq"}, {dk, "dk"}, {dq_weight, "dq_weight"}, {dk_weight, "dk_weight"}};
+  const Named ins[] = {{dq_out, "dq_out"}, {dk_out, "dk_out"}, {q, "q"}, {k, "k"}, {norm.q_weight, "q_weight"},
+                       {norm.k_weight, "k_weight"}};
+  const rl_tensor* same[] = {dq_out, dk_out, nullptr, nullptr};
+  RL_TRY(check_apart(outs, same, 4, ins, 6));
+  int cus = 0;
+  RL_TRY(current_cus(&cus));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const size_t need = rope_grad_bytes(cus);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, need, need, false, &w));
+  rope_grad_groups(rows, Hq, Hkv, cus, &g.q_groups, &g.k_groups);
+  a.q = q->data;
+  a.q_st = q->strides[0];
+  a.q_sh = q->strides[1];
+  a.q_out = dq->data;
+  a.qo_st = dq->strides[0];
+  a.qo_sh = dq->strides[1];
+  g.dq_out = dq_out->data;
+  g.gq_st = dq_out->strides[0];
+  g.gq_sh = dq_out->strides[1];
+  g.dq_weight = static_cast<float*>(dq_weight->data);
+  g.dqw_s = dq_weight->strides[0];
+  if (k) {
+    a.k = k->data;
+    a.k_st = k->strides[0];
+    a.k_sh = k->strides[1];
+    a.k_out = dk->data;
+    a.ko_st = dk->strides[0];
+    a.ko_sh = dk->strides[1];
+    g.dk_out = dk_out->data;
+    g.gk_st = dk_out->strides[0];
+    g.gk_sh = dk_out->strides[1];
+    g.dk_weight = static_cast<float*>(dk_weight->data);
+    g.dkw_s = dk_weight->strides[0];
+  }
+  g.parts = static_cast<float*>(w->ptr);
+  a.rows = (int)rows;
+  a.Hq = (int)Hq;
+  a.Hkv = (int)Hkv;
+  a.err = w->err;
+  rl::KernelTimer slot;
+  rl::KernelTimer* timer = prof_timer(&slot, st);
+  const hipError_t e = rl::launch_rope_grad(g, st, timer);
+  prof_commit(4, timer);
+  if (e != hipSuccess) return hip_fail(e, "rotary gradient kernel launch");
+  return RL_OK;
+}
+
+// ----------------------------------------------------------- log probabilities
+// A matrix of logits [rows, vocab], bf16 or f32, its rows contiguous; any alignment of an element.
+int check_logits(const rl_tensor* t, const char* name, bool written) {
+  RL_TRY(check_view(t, name, 2));
+  if (t->dtype != RL_BF16 && t->dtype != RL_F32)
+    return fail(RL_ERR_DTYPE, "%s must be bf16 or f32 (got %s)", name, dtype_name(t->dtype));
+  if (t->shape[1] > 1 && t->strides[1] != 1) return fail(RL_ERR_UNSUPPORTED, "%s: last stride must be 1", name);
+  if (t->strides[0] < 0 || (written && t->shape[0] > 1 && t->strides[0] < t->shape[1]))
+    return fail(RL_ERR_UNSUPPORTED, "%s: the row stride must be non-negative%s", name,
+                written ? ", and rows that are written must not overlap" : "");
+  if (reinterpret_cast<uintptr_t>(t->data) % elem_bytes(t->dtype) != 0)
+    return fail(RL_ERR_UNSUPPORTED, "%s: data must be aligned to its elements", name);
+  return check_data(t, name);
+}
+// (as rows of one run each)
+rl_tensor as_runs(const rl_tensor* t) {
+  rl_tensor r = *t;
+  r.ndim = 3;
+  r.shape[2] = t->shape[1];
+  r.shape[1] = 1;
+  r.strides[1] = 0;
+  return r;
+}
+int check_row_floats(const rl_tensor* t, const char* name, int64_t rows, bool written) {
+  return t ? check_vector(t, name, RL_F32, rows, written) : RL_OK;
+}
+
+// What a call and its gradient have in common.
+int fill_logprobs(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale, rl::LogprobArgs* a) {
+  RL_TRY(check_logits(logits, "logits", false));
+  const int64_t rows = logits->shape[0], vocab = logits->shape[1];
+  if (vocab < 1) return fail(RL_ERR_SHAPE, "logits must have at least one column");
+  if (vocab > (1 << 21) || rows >= (1 << 24)) return fail(RL_ERR_UNSUPPORTED, "vocabulary or rows too large");
+  RL_TRY(check_view(tokens, "tokens", 1));
+  if (tokens->dtype != RL_I32 && tokens->dtype != RL_I64)
+    return fail(RL_ERR_DTYPE, "tokens must be int32 or int64 (got %s)", dtype_name(tokens->dtype));
+  RL_TRY(check_vector(tokens, "tokens", tokens->dtype, rows, false));
+  if (row_scale) RL_TRY(check_vector(row_scale, "row_scale", RL_F32, rows, false));
+  a->x = logits->data;
+  a->x_s = logits->strides[0];
+  a->f32 = logits->dtype == RL_F32;
+  a->tokens = tokens->data;
+  a->tok_s = tokens->strides[0];
+  a->tok64 = tokens->dtype == RL_I64;
+  a->scale = row_scale ? static_cast<const float*>(row_scale->data) : nullptr;
+  a->scale_s = row_scale ? row_scale->strides[0] : 0;
+  a->rows = (int)rows;
+  a->vocab = (int)vocab;
+  return RL_OK;
+}
+
+// Sums of the segments of rows that several workgroups have, and those workgroups' likeliest tokens.
+struct LogprobLayout {
+  size_t cands, total;
+};
+LogprobLayout logprob_layout(int64_t rows, int64_t vocab, int64_t chunks, int64_t top) {
+  const int64_t segs = (vocab + rl::kLogprobSegment - 1) / rl::kLogprobSegment;
+  LogprobLayout l{};
+  l.cands = align256((size_t)(rows * segs * rl::kLogprobPartBytes));
+  l.total = l.cands + (size_t)(rows * chunks * top * 8);
+  return l;
+}
+
+int logprobs_impl(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale, rl_tensor* logprobs,
+                  rl_tensor* entropy, rl_tensor* lse, rl_tensor* top_ids, rl_tensor* top_logprobs, void* stream) {
+  rl::LogprobArgs a{};
+  RL_TRY(fill_logprobs(logits, tokens, row_scale, &a));
+  const int64_t rows = a.rows;
+  RL_TRY(check_vector(logprobs, "logprobs", RL_F32, rows, true));
+  RL_TRY(check_row_floats(entropy, "entropy", rows, true));
+  RL_TRY(check_row_floats(lse, "lse", rows, true));
+  if ((top_ids != nullptr) != (top_logprobs != nullptr))
+    return fail(RL_ERR_INVALID_ARG, "top_ids and top_logprobs must be given together");
+  if (top_ids) {
+    RL_TRY(check_view(top_ids, "top_ids", 2));
+    const int64_t top = top_ids->shape[1];
+    for (const Named& t : {Named{top_ids, "top_ids"}, Named{top_logprobs, "top_logprobs"}}) {
+      RL_TRY(check_view(t.t, t.name, 2));
+      RL_TRY(check_dtype(t.t, t.name, t.t == top_ids ? RL_I32 : RL_F32));
+      if (t.t->shape[0] != rows || t.t->shape[1] != top)
+        return fail(RL_ERR_SHAPE, "%s must be [%lld, %lld]", t.name, (long long)rows, (long long)top);
+      if ((top > 1 && t.t->strides[1] != 1) || t.t->strides[0] < 0)
+        return fail(RL_ERR_UNSUPPORTED, "%s: last stride must be 1, the row stride non-negative", t.name);
+      RL_TRY(check_data(t.t, t.name));
+    }
+    if (top > rl::kLogprobTop)
+      return fail(RL_ERR_UNSUPPORTED, "at most %d alternatives (got %lld)", rl::kLogprobTop, (long long)top);
+    a.top = (int)top;
+  }
+  if (rows == 0) return RL_OK;
+  const rl_tensor x = as_runs(logits);
+  const Named outs[] = {{logprobs, "logprobs"}, {entropy, "entropy"}, {lse, "lse"}, {top_ids, "top_ids"},
+                        {top_logprobs, "top_logprobs"}};
+  const Named ins[] = {{&x, "logits"}, {tokens, "tokens"}, {row_scale, "row_scale"}};
+  const rl_tensor* same[5] = {};
+  RL_TRY(check_apart(outs, same, 5, ins, 3));
+  int cus = 0;
+  RL_TRY(current_cus(&cus));
+  a.chunks = rl::logprob_chunks(rows, a.vocab, cus);
+  if (rows * a.chunks >= (1 << 24)) return fail(RL_ERR_UNSUPPORTED, "rows too many");
+  const LogprobLayout l = logprob_layout(rows, a.vocab, a.chunks, a.top);
+  const size_t need = a.chunks > 1 ? l.total : 0;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, need, need, false, &w));
+  a.parts = w->ptr;
+  a.cands = need ? reinterpret_cast<uint64_t*>(static_cast<char*>(w->ptr) + l.cands) : nullptr;
+  a.logprobs = static_cast<float*>(logprobs->data);
+  a.lp_s = logprobs->strides[0];
+  a.entropy = entropy ? static_cast<float*>(entropy->data) : nullptr;
+  a.ent_s = entropy ? entropy->strides[0] : 0;
+  a.lse = lse ? static_cast<float*>(lse->data) : nullptr;
+  a.lse_s = lse ? lse->strides[0] : 0;
+  if (a.top > 0) {
+    a.top_ids = static_cast<int*>(top_ids->data);
+    a.ti_s = top_ids->strides[0];
+    a.top_lps = static_cast<float*>(top_logprobs->data);
+    a.tl_s = top_logprobs->strides[0];
+  }
+  a.err = w->err;
+  const hipError_t e = rl::launch_logprob(a, st);
+  if (e != hipSuccess) return hip_fail(e, "log probability kernel launch");
+  return RL_OK;
+}
+
+int logprobs_grad_impl(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale,
+                       const rl_tensor* lse, const rl_tensor* entropy, const rl_tensor* d_logprobs,
+                       const rl_tensor* d_entropy, rl_tensor* d_logits, void* stream) {
+  rl::LogprobArgs a{};
+  RL_TRY(fill_logprobs(logits, tokens, row_scale, &a));
+  const int64_t rows = a.rows;
+  RL_TRY(check_vector(lse, "lse", RL_F32, rows, false));
+  RL_TRY(check_row_floats(d_logprobs, "d_logprobs", rows, false));
+  RL_TRY(check_row_floats(d_entropy, "d_entropy", rows, false));
+  if (!d_logprobs && !d_entropy) return fail(RL_ERR_INVALID_ARG, "d_logprobs and d_entropy are both NULL");
+  if (d_entropy) RL_TRY(check_vector(entropy, "entropy", RL_F32, rows, false));
+  RL_TRY(check_logits(d_logits, "d_logits", true));
+  RL_TRY(check_dtype(d_logits, "d_logits", logits->dtype));
+  if (d_logits->shape[0] != rows || d_logits->shape[1] != a.vocab)
+    return fail(RL_ERR_SHAPE, "d_logits must be [%lld, %lld]", (long long)rows, (long long)a.vocab);
+  // (a launch has fewer than 2^32 threads, 256 for 4096 logits)
+  if (rows * ((a.vocab + 4095) / 4096) >= (1 << 24)) return fail(RL_ERR_UNSUPPORTED, "rows times vocabulary too large");
+  if (rows == 0) return RL_OK;
+  const rl_tensor x = as_runs(logits), d = as_runs(d_logits);
+  const Named outs[] = {{&d, "d_logits"}};
+  const Named ins[] = {{&x, "logits"}, {tokens, "tokens"}, {row_scale, "row_scale"}, {lse, "lse"},
+                       {entropy, "entropy"}, {d_logprobs, "d_logprobs"}, {d_entropy, "d_entropy"}};
+  const rl_tensor* same[] = {&x};
+  RL_TRY(check_apart(outs, same, 1, ins, 7));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
+  a.lse = static_cast<float*>(lse->data);
+  a.lse_s = lse->strides[0];
+  a.entropy = d_entropy ? static_cast<float*>(entropy->data) : nullptr;
+  a.ent_s = d_entropy ? entropy->strides[0] : 0;
+  a.d_lp = d_logprobs ? static_cast<const float*>(d_logprobs->data) : nullptr;
+  a.dlp_s = d_logprobs ? d_logprobs->strides[0] : 0;
+  a.d_ent = d_entropy ? static_cast<const float*>(d_entropy->data) : nullptr;
+  a.dent_s = d_entropy ? d_entropy->strides[0] : 0;
+  a.d_x = d_logits->data;
+  a.dx_s = d_logits->strides[0];
+  a.err = w->err;
+  const hipError_t e = rl::launch_logprob_grad(a, st);
+  if (e != hipSuccess) return hip_fail(e, "log probability gradient kernel launch");
+  return RL_OK;
+}
+
+// ------------------------------------------------- requests that begin and end
+// The pool's sizes and a block table of B requests, as the slot maps take them.
+int check_table(const rl_tensor* block_table, int64_t B, int64_t free_pages, int64_t page_size, int64_t num_pages,
+                bool written) {
+  if (page_size < 8 || page_size > 128 || (page_size & (page_size - 1)) != 0)
+    return fail(RL_ERR_UNSUPPORTED, "page size must be a power of two in [8, 128] (got %lld)", (long long)page_size);
+  if (num_pages < 0) return fail(RL_ERR_INVALID_ARG, "num_pages is negative");
+  RL_TRY(check_view(block_table, "block_table", 2));
+  RL_TRY(check_dtype(block_table, "block_table", RL_I32));
+  if (block_table->shape[0] != B)
+    return fail(RL_ERR_SHAPE, "block_table.shape[0] (%lld) != batch (%lld)", (long long)block_table->shape[0],
+                (long long)B);
+  const int64_t max_pages = block_table->shape[1], lim24 = (int64_t)1 << 24;
+  if (num_pages > INT32_MAX || free_pages > INT32_MAX || max_pages >= lim24 || max_pages * page_size > INT32_MAX)
+    return fail(RL_ERR_UNSUPPORTED, "page pool or block table too large for 32-bit token indices");
+  if (block_table->strides[0] < 0 || block_table->strides[1] < 0 || block_table->strides[1] >= lim24 ||
+      (written && ((B > 0 && max_pages > 1 && block_table->strides[1] < 1) ||
+                   (B > 1 && max_pages > 0 && block_table->strides[0] < 1))))
+    return fail(RL_ERR_UNSUPPORTED, "block_table: strides must be positive, the column stride below 2^24");
+  return check_data(block_table, "block_table");
+}
+
+int fork_impl(const rl_tensor* parents, const rl_tensor* fork_lens, const rl_tensor* kv_lens,
+              const rl_tensor* free_pages, const rl_tensor* free_used, int64_t page_size, int64_t num_pages,
+              rl_tensor* block_table, rl_tensor* kv_lens_out, rl_tensor* free_used_out, rl_tensor* copies,
+              void* stream) {
+  RL_TRY(check_view(kv_lens, "kv_lens", 1));
+  const int64_t B = kv_lens->shape[0];
+  if (B > (1 << 22)) return fail(RL_ERR_UNSUPPORTED, "batch too large");
+  RL_TRY(check_vector(parents, "parents", RL_I32, B, false));
+  RL_TRY(check_vector(fork_lens, "fork_lens", RL_I32, B, false));
+  RL_TRY(check_vector(kv_lens, "kv_lens", RL_I32, B, false));
+  RL_TRY(check_view(free_pages, "free_pages", 1));
+  RL_TRY(check_vector(free_pages, "free_pages", RL_I32, free_pages->shape[0], false));
+  RL_TRY(check_vector(free_used, "free_used", RL_I32, 1, false));
+  RL_TRY(check_table(block_table, B, free_pages->shape[0], page_size, num_pages, true));
+  RL_TRY(check_vector(kv_lens_out, "kv_lens_out", RL_I32, B, true));
+  RL_TRY(check_vector(free_used_out, "free_used_out", RL_I32, 1, true));
+  RL_TRY(check_view(copies, "copies", 2));
+  RL_TRY(check_dtype(copies, "copies", RL_I32));
+  if (copies->shape[0] != B || copies->shape[1] != 3)
+    return fail(RL_ERR_SHAPE, "copies must be [%lld, 3]", (long long)B);
+  if (copies->strides[1] != 1 || copies->strides[0] < 0)
+    return fail(RL_ERR_UNSUPPORTED, "copies: last stride must be 1, the row stride non-negative");
+  RL_TRY(check_data(copies, "copies"));
+  const Named outs[] = {{block_table, "block_table"}, {kv_lens_out, "kv_lens_out"}, {free_used_out, "free_used_out"},
+                        {copies, "copies"}};
+  const rl_tensor* same[] = {nullptr, kv_lens, free_used, nullptr};
+  const Named ins[] = {{parents, "parents"}, {fork_lens, "fork_lens"}, {kv_lens, "kv_lens"},
+                       {free_pages, "free_pages"}, {free_used, "free_used"}};
+  RL_TRY(check_apart(outs, same, 4, ins, 5));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
+  rl::ForkArgs a{};
+  a.parents = static_cast<const int*>(parents->data);
+  a.fork_lens = static_cast<const int*>(fork_lens->data);
+  a.kv_lens = static_cast<const int*>(kv_lens->data);
+  a.free_pages = static_cast<const int*>(free_pages->data);
+  a.free_used = static_cast<const int*>(free_used->data);
+  a.par_s = parents->strides[0];
+  a.fl_s = fork_lens->strides[0];
+  a.kv_s = kv_lens->strides[0];
+  a.free_s = free_pages->strides[0];
+  a.bt = static_cast<int*>(block_table->data);
+  a.bt_sb = block_table->strides[0];
+  a.bt_sj = block_table->strides[1];
+  a.kv_out = static_cast<int*>(kv_lens_out->data);
+  a.used_out = static_cast<int*>(free_used_out->data);
+  a.copies = static_cast<int*>(copies->data);
+  a.kv_out_s = kv_lens_out->strides[0];
+  a.cp_s = copies->strides[0];
+  a.B = (int)B;
+  a.n_free = (int)free_pages->shape[0];
+  a.num_pages = (int)num_pages;
+  a.page_size = (int)page_size;
+  while ((1 << a.log2_page) < page_size) ++a.log2_page;
+  a.max_pages = (int)block_table->shape[1];
+  a.err = w->err;
+  const hipError_t e = rl::launch_fork(a, st);
+  if (e != hipSuccess) return hip_fail(e, "fork kernel launch");
+  return RL_OK;
+}
+
+int copy_pages_impl(const rl_tensor* copies, rl_tensor* k_pages, rl_tensor* v_pages, void* stream) {
+  RL_TRY(check_view(copies, "copies", 2));
+  RL_TRY(check_dtype(copies, "copies", RL_I32));
+  if (copies->shape[1] != 3) return fail(RL_ERR_SHAPE, "copies must be [n, 3]");
+  if (copies->strides[1] != 1 || copies->strides[0] < 0)
+    return fail(RL_ERR_UNSUPPORTED, "copies: last stride must be 1, the row stride non-negative");
+  RL_TRY(check_data(copies, "copies"));
+  RL_TRY(check_view(k_pages, "k_pages", 4));
+  const int dtype = k_pages->dtype;
+  if (dtype != RL_BF16 && dtype != RL_FP8_E4M3)
+    return fail(RL_ERR_DTYPE, "k_pages must be bf16 or fp8_e4m3 (got %s)", dtype_name(dtype));
+  RL_TRY(check_view(v_pages, "v_pages", 4));
+  RL_TRY(check_dtype(v_pages, "v_pages", dtype));
+  const int64_t e = elem_bytes(dtype);
+  for (const Named& t : {Named{k_pages, "k_pages"}, Named{v_pages, "v_pages"}}) {
+    RL_TRY(check_rows128(t.t, t.name));
+    for (int i = 0; i < 3; ++i) {
+      if (t.t->shape[i] != k_pages->shape[i]) return fail(RL_ERR_SHAPE, "k_pages and v_pages shapes differ");
+      if (t.t->strides[i] * e % 16 != 0)
+        return fail(RL_ERR_UNSUPPORTED, "%s: stride[%d] must be a multiple of 16 bytes", t.name, i);
+    }
+    RL_TRY(check_data(t.t, t.name));
+  }
+  const int64_t n = copies->shape[0], P = k_pages->shape[1], Hkv = k_pages->shape[2];
+  if (P < 8 || P > 128 || (P & (P - 1)) != 0)
+    return fail(RL_ERR_UNSUPPORTED, "page size must be a power of two in [8, 128] (got %lld)", (long long)P);
+  if (k_pages->shape[0] > INT32_MAX || Hkv > 4096) return fail(RL_ERR_UNSUPPORTED, "page pool or head count too large");
+  // (a launch has fewer than 2^32 threads, 512 for 16 KB of a page)
+  if (n * ((P * Hkv * 128 * e + 16383) / 16384) >= (1 << 23)) return fail(RL_ERR_UNSUPPORTED, "copies too many");
+  if (n == 0 || Hkv == 0) return RL_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
+  rl::CopyArgs a{};
+  a.copies = static_cast<const int*>(copies->data);
+  a.cp_s = copies->strides[0];
+  a.k = static_cast<char*>(k_pages->data);
+  a.v = static_cast<char*>(v_pages->data);
+  a.kp_sp = k_pages->strides[0] * e;
+  a.kp_ss = k_pages->strides[1] * e;
+  a.kp_sh = k_pages->strides[2] * e;
+  a.vp_sp = v_pages->strides[0] * e;
+  a.vp_ss = v_pages->strides[1] * e;
+  a.vp_sh = v_pages->strides[2] * e;
+  a.n = (int)n;
+  a.Hkv = (int)Hkv;
+  a.row_bytes = (int)(128 * e);
+  a.num_pages = (int)k_pages->shape[0];
+  a.page_size = (int)P;
+  a.err = w->err;
+  const hipError_t err = rl::launch_copy_pages(a, st);
+  if (err != hipSuccess) return hip_fail(err, "page copy kernel launch");
+  return RL_OK;
+}
+
+int drop_impl(const rl_tensor* kv_lens, const rl_tensor* keep_lens, const rl_tensor* block_table, int64_t page_size,
+              int64_t num_pages, rl_tensor* free_pages, const rl_tensor* free_used, rl_tensor* kv_lens_out,
+              rl_tensor* free_used_out, void* stream) {
+  RL_TRY(check_view(kv_lens, "kv_lens", 1));
+  const int64_t B = kv_lens->shape[0];
+  if (B > (1 << 22)) return fail(RL_ERR_UNSUPPORTED, "batch too large");
+  RL_TRY(check_vector(kv_lens, "kv_lens", RL_I32, B, false));
+  RL_TRY(check_vector(keep_lens, "keep_lens", RL_I32, B, false));
+  RL_TRY(check_view(free_pages, "free_pages", 1));
+  RL_TRY(check_vector(free_pages, "free_pages", RL_I32, free_pages->shape[0], true));
+  RL_TRY(check_vector(free_used, "free_used", RL_I32, 1, false));
+  RL_TRY(check_table(block_table, B, free_pages->shape[0], page_size, num_pages, false));
+  RL_TRY(check_vector(kv_lens_out, "kv_lens_out", RL_I32, B, true));
+  RL_TRY(check_vector(free_used_out, "free_used_out", RL_I32, 1, true));
+  const Named outs[] = {{free_pages, "free_pages"}, {kv_lens_out, "kv_lens_out"}, {free_used_out, "free_used_out"}};
+  const rl_tensor* same[] = {nullptr, kv_lens, free_used};
+  const Named ins[] = {{kv_lens, "kv_lens"}, {keep_lens, "keep_lens"}, {block_table, "block_table"},
+                       {free_used, "free_used"}};
+  RL_TRY(check_apart(outs, same, 3, ins, 4));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Workspace* w = nullptr;
+  RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
+  rl::DropArgs a{};
+  a.kv_lens = static_cast<const int*>(kv_lens->data);
+  a.keep_lens = static_cast<const int*>(keep_lens->data);
+  a.bt = static_cast<const int*>(block_table->data);
+  a.kv_s = kv_lens->strides[0];
+  a.keep_s = keep_lens->strides[0];
+  a.bt_sb = block_table->strides[0];
+  a.bt_sj = block_table->strides[1];
+  a.free_pages = static_cast<int*>(free_pages->data);
+  a.free_used = static_cast<const int*>(free_used->data);
+  a.free_s = free_pages->strides[0];
+  a.kv_out = static_cast<int*>(kv_lens_out->data);
+  a.used_out = static_cast<int*>(free_used_out->data);
+  a.kv_out_s = kv_lens_out->strides[0];
+  a.B = (int)B;
+  a.n_free = (int)free_pages->shape[0];
+  a.num_pages = (int)num_pages;
+  a.page_size = (int)page_size;
+  while ((1 << a.log2_page) < page_size) ++a.log2_page;
+  a.max_pages = (int)block_table->shape[1];
+  a.err = w->err;
+  const hipError_t e = rl::launch_drop(a, st);
+  if (e != hipSuccess) return hip_fail(e, "drop kernel launch");
   return RL_OK;
 }
 
@@ -1497,7 +1989,7 @@ int rl_attn_map_slots(const rl_tensor* kv_lens, const rl_tensor* new_lens, const
 
 int rl_attn_rope(const rl_tensor* q, const rl_tensor* k, const rl_tensor* positions, const rl_tensor* inv_freq,
                  const rl_tensor* axes, const rl_rope_opts* opts, rl_tensor* q_out, rl_tensor* k_out, void* stream) {
-  return rope_impl(q, k, nullptr, positions, inv_freq, axes, opts, nullptr, q_out, k_out, nullptr, nullptr, false,
+  return rope_impl(q, k, nullptr, nullptr, positions, inv_freq, axes, opts, nullptr, q_out, k_out, nullptr, nullptr, false,
                    RL_BF16, nullptr, nullptr, stream);
 }
 
@@ -1505,7 +1997,7 @@ int rl_attn_rope_append_kv(const rl_tensor* q, const rl_tensor* k_new, const rl_
                            const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
                            const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out, rl_tensor* k_out,
                            rl_tensor* k_pages, rl_tensor* v_pages, void* stream) {
-  return rope_impl(q, k_new, v_new, positions, inv_freq, axes, opts, slot_map, q_out, k_out, k_pages, v_pages, true,
+  return rope_impl(q, k_new, v_new, nullptr, positions, inv_freq, axes, opts, slot_map, q_out, k_out, k_pages, v_pages, true,
                    RL_BF16, nullptr, nullptr, stream);
 }
 
@@ -1514,8 +2006,77 @@ int rl_attn_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const
                                const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out,
                                rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, const rl_tensor* k_scale,
                                const rl_tensor* v_scale, void* stream) {
-  return rope_impl(q, k_new, v_new, positions, inv_freq, axes, opts, slot_map, q_out, k_out, k_pages, v_pages, true,
+  return rope_impl(q, k_new, v_new, nullptr, positions, inv_freq, axes, opts, slot_map, q_out, k_out, k_pages, v_pages, true,
                    RL_FP8_E4M3, k_scale, v_scale, stream);
+}
+
+int rl_attn_norm_rope(const rl_tensor* q, const rl_tensor* k, const rl_tensor* q_weight, const rl_tensor* k_weight,
+                      float eps, const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                      const rl_rope_opts* opts, rl_tensor* q_out, rl_tensor* k_out, void* stream) {
+  const Norm norm{q_weight, k_weight, eps};
+  return rope_impl(q, k, nullptr, &norm, positions, inv_freq, axes, opts, nullptr, q_out, k_out, nullptr, nullptr,
+                   false, RL_BF16, nullptr, nullptr, stream);
+}
+
+int rl_attn_norm_rope_append_kv(const rl_tensor* q, const rl_tensor* k_new, const rl_tensor* v_new,
+                                const rl_tensor* q_weight, const rl_tensor* k_weight, float eps,
+                                const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                                const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out,
+                                rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, void* stream) {
+  const Norm norm{q_weight, k_weight, eps};
+  return rope_impl(q, k_new, v_new, &norm, positions, inv_freq, axes, opts, slot_map, q_out, k_out, k_pages, v_pages,
+                   true, RL_BF16, nullptr, nullptr, stream);
+}
+
+int rl_attn_norm_rope_append_kv_fp8(const rl_tensor* q, const rl_tensor* k_new, const rl_tensor* v_new,
+                                    const rl_tensor* q_weight, const rl_tensor* k_weight, float eps,
+                                    const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                                    const rl_rope_opts* opts, const rl_tensor* slot_map, rl_tensor* q_out,
+                                    rl_tensor* k_out, rl_tensor* k_pages, rl_tensor* v_pages, const rl_tensor* k_scale,
+                                    const rl_tensor* v_scale, void* stream) {
+  const Norm norm{q_weight, k_weight, eps};
+  return rope_impl(q, k_new, v_new, &norm, positions, inv_freq, axes, opts, slot_map, q_out, k_out, k_pages, v_pages,
+                   true, RL_FP8_E4M3, k_scale, v_scale, stream);
+}
+
+int rl_attn_norm_rope_backward(const rl_tensor* dq_out, const rl_tensor* dk_out, const rl_tensor* q,
+                               const rl_tensor* k, const rl_tensor* q_weight, const rl_tensor* k_weight, float eps,
+                               const rl_tensor* positions, const rl_tensor* inv_freq, const rl_tensor* axes,
+                               const rl_rope_opts* opts, rl_tensor* dq, rl_tensor* dk, rl_tensor* dq_weight,
+                               rl_tensor* dk_weight, void* stream) {
+  return rope_grad_impl(dq_out, dk_out, q, k, Norm{q_weight, k_weight, eps}, positions, inv_freq, axes, opts, dq, dk,
+                        dq_weight, dk_weight, stream);
+}
+
+int rl_attn_token_logprobs(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale,
+                           rl_tensor* logprobs, rl_tensor* entropy, rl_tensor* lse, rl_tensor* top_ids,
+                           rl_tensor* top_logprobs, void* stream) {
+  return logprobs_impl(logits, tokens, row_scale, logprobs, entropy, lse, top_ids, top_logprobs, stream);
+}
+
+int rl_attn_token_logprobs_backward(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale,
+                                    const rl_tensor* lse, const rl_tensor* entropy, const rl_tensor* d_logprobs,
+                                    const rl_tensor* d_entropy, rl_tensor* d_logits, void* stream) {
+  return logprobs_grad_impl(logits, tokens, row_scale, lse, entropy, d_logprobs, d_entropy, d_logits, stream);
+}
+
+int rl_attn_fork_requests(const rl_tensor* parents, const rl_tensor* fork_lens, const rl_tensor* kv_lens,
+                          const rl_tensor* free_pages, const rl_tensor* free_used, int64_t page_size,
+                          int64_t num_pages, rl_tensor* block_table, rl_tensor* kv_lens_out, rl_tensor* free_used_out,
+                          rl_tensor* copies, void* stream) {
+  return fork_impl(parents, fork_lens, kv_lens, free_pages, free_used, page_size, num_pages, block_table, kv_lens_out,
+                   free_used_out, copies, stream);
+}
+
+int rl_attn_copy_pages(const rl_tensor* copies, rl_tensor* k_pages, rl_tensor* v_pages, void* stream) {
+  return copy_pages_impl(copies, k_pages, v_pages, stream);
+}
+
+int rl_attn_drop_tokens(const rl_tensor* kv_lens, const rl_tensor* keep_lens, const rl_tensor* block_table,
+                        int64_t page_size, int64_t num_pages, rl_tensor* free_pages, const rl_tensor* free_used,
+                        rl_tensor* kv_lens_out, rl_tensor* free_used_out, void* stream) {
+  return drop_impl(kv_lens, keep_lens, block_table, page_size, num_pages, free_pages, free_used, kv_lens_out,
+                   free_used_out, stream);
 }
 
 int rl_attn_prefill(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const rl_tensor* seq_indptr,
@@ -1619,6 +2180,9 @@ int rl_attn_check_device_errors(void* stream) {
     if (word & rl::kErrPool) what += " free-pages-exhausted";
     if (word & rl::kErrSlot) what += " slot-out-of-range";
     if (word & rl::kErrAxis) what += " position-axis-out-of-range";
+    if (word & rl::kErrToken) what += " token-out-of-range";
+    if (word & rl::kErrRowScale) what += " row-scale-invalid";
+    if (word & rl::kErrParent) what += " fork-invalid";
     return fail(RL_ERR_DEVICE, "device-side input errors (values were clamped):%s", what.c_str());
   }
   return RL_OK;
@@ -1663,6 +2227,23 @@ size_t rl_attn_extend_workspace_size(int64_t batch, int64_t total_q, int64_t num
   if (hipGetDevice(&dev) == hipSuccess) cus = device_cus(dev);
   return extend_layout(batch, total_q, total_q, num_kv_heads, num_q_heads / num_kv_heads, max_pages * page_size, cus)
       .total;
+}
+
+size_t rl_attn_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int64_t top) {
+  if (rows <= 0 || vocab <= 0 || vocab > (1 << 21) || top < 0 || top > rl::kLogprobTop) return 0;
+  int dev = 0, cus = 256;
+  if (hipGetDevice(&dev) == hipSuccess) cus = device_cus(dev);
+  // only rows that one workgroup each would not fill the device with are shared
+  // out, fewer than 8 a CU, over less than twice as many workgroups
+  const int64_t some = std::min<int64_t>(rows, 8 * (int64_t)cus), segs = (vocab + 4095) / 4096;
+  return align256((size_t)(some * segs * rl::kLogprobPartBytes)) +
+         (size_t)(std::min<int64_t>(some * rl::kLogprobChunks, 16 * (int64_t)cus) * top * 8);
+}
+
+size_t rl_attn_norm_rope_backward_workspace_size(void) {
+  int dev = 0, cus = 256;
+  if (hipGetDevice(&dev) == hipSuccess) cus = device_cus(dev);
+  return rope_grad_bytes(cus);
 }
 
 // ------------------------------------------------------------ measurement aids

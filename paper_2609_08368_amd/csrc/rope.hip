@@ -33,9 +33,8 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "attn_common.hpp"
-#include "e4m3.hpp"
 #include "kernels.hpp"
+#include "rope_rows.hpp"
 
 namespace rl {
 
@@ -44,98 +43,9 @@ namespace {
 constexpr int kRopeThreads = 256;
 constexpr int kWavesPerCu = 32;                     // that fit at once
 
-// cos and sin of 2 pi t for t in turns, any size: t is reduced in 64 bits to
-// x in [-1/8, 1/8] turns around a quarter k, and |2 pi x| <= pi/4 leaves the
-// first dropped Taylor terms below 2e-9 (sine) and 2e-9 (cosine).
-__device__ __forceinline__ float2 cos_sin_turns(double t) {
-  const double r = t - __builtin_rint(t);           // [-1/2, 1/2]
-  const double k4 = __builtin_rint(4.0 * r);        // quarter, -2..2
-  const float y = (float)((r - 0.25 * k4) * 6.283185307179586476925);
-  const int k = (int)k4 & 3;
-  const float z = y * y;
-  const float s = y * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), 1.f);
-  const float c = fmaf(
-      z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
-  const float a = (k & 1) ? s : c, b = (k & 1) ? c : s;
-  // quarter 0: (c, s), 1: (-s, c), 2: (-c, -s), 3: (s, -c)
-  return {(k == 1 || k == 2) ? -a : a, (k >= 2) ? -b : b};
-}
-
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ f32x8 widen(bf16x8 x) {
-  f32x8 y;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = (float)x[e];
-  return y;
-}
-__device__ __forceinline__ bf16x8 narrow(f32x8 x) {
-  bf16x8 y;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[e];
-  return y;
-}
-__device__ __forceinline__ uint2 codes(f32x8 x, float s, float inv) {
-  float f[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = x[e];
-  return e4m3_pack8(f, s, inv);
-}
-
-// First elements of the two chunks of duplet d: with F frequencies, duplets
-// below F / 8 are rotated, the others hold 16 neighbours behind them.
-struct Chunks {
-  int lo, hi;
-  bool turned;
-};
-__device__ __forceinline__ Chunks chunks_of(int d, int F, bool interleaved) {
-  const bool turned = 8 * d < F;
-  if (turned && !interleaved) return {8 * d, F + 8 * d, true};
-  return {16 * d, 16 * d + 8, turned};
-}
-
-// cs: cos and sin of the duplet's eight frequencies. (x cos a - y sin a, y cos a +
-// x sin a), with the fused products written out: left to the compiler they differ
-// between the kernels, and a row's bits with the size of its call.
-__device__ __forceinline__ void turn_pair(float& x, float& y, float2 cs) {
-  const float u = x, w = y;
-  x = fmaf(u, cs.x, -(w * cs.y));
-  y = fmaf(w, cs.x, u * cs.y);
-}
-__device__ __forceinline__ void turn(f32x8& a, f32x8& b, const float2 (&cs)[8], bool interleaved) {
-  if (interleaved) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      f32x8& z = e < 4 ? a : b;
-      const int i = 2 * (e & 3);
-      float x = z[i], y = z[i + 1];
-      turn_pair(x, y, cs[e]);
-      z[i] = x;
-      z[i + 1] = y;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float x = a[e], y = b[e];
-      turn_pair(x, y, cs[e]);
-      a[e] = x;
-      b[e] = y;
-    }
-  }
-}
-
-template <bool kNt, typename T>
-__device__ __forceinline__ void store_chunk(void* dst, T x) {
-  typedef unsigned int words __attribute__((ext_vector_type(sizeof(T) / 4)));
-  if constexpr (kNt)
-    __builtin_nontemporal_store(__builtin_bit_cast(words, x), static_cast<words*>(dst));
-  else
-    *static_cast<words*>(dst) = __builtin_bit_cast(words, x);
-}
-
 // A wave has eight head rows of a row (kLarge: sixteen, stored nontemporally),
 // which it loads before it forms the row's angles.
-template <bool kAppend, bool kFp8, bool kLarge>
+template <bool kAppend, bool kFp8, bool kLarge, bool kNorm>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
   constexpr int kBatch = kLarge ? 2 : 1;            // eights of head rows
   __shared__ __attribute__((aligned(16))) float2 cs[kRopeThreads / 64][64];
@@ -199,6 +109,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
     const int kind = kind_of(h), g = h - a.Hq - (kind == kV ? a.Hkv : 0);   // g: KV head
     const Chunks c = kind == kV ? plain : turned;
     f32x8 fa = widen(xa[i]), fb = widen(xb[i]);
+    if (kNorm && kind != kV) {
+      const void* w = kind == kQ ? a.q_weight : a.k_weight;
+      const float rms = inv_rms(fa, fb, a.eps);
+      fa = fa * rms * load_weights(w, c.lo, a.weights_f32);
+      fb = fb * rms * load_weights(w, c.hi, a.weights_f32);
+    }
     if (c.turned) turn(fa, fb, t, a.interleaved);
     if (kind == kQ || (kind == kK && a.k_out)) {
       __bf16* dst = kind == kK ? (__bf16*)a.k_out + r * a.ko_st + g * a.ko_sh
@@ -237,11 +153,17 @@ hipError_t launch_rope(const RopeArgs& args, int cus, hipStream_t stream, Kernel
   const bool large = a.rows * eights > (int64_t)kWavesPerCu * cus;
   a.parts = (int)(large ? (eights + 1) / 2 : eights);
   const unsigned grid = (unsigned)(((int64_t)a.rows * a.parts + kRopeThreads / 64 - 1) / (kRopeThreads / 64));
-  auto run = [&](auto append, auto fp8) {
+  auto launch = [&](auto append, auto fp8, auto norm) {
     if (large)
-      rope_kernel<append, fp8, true><<<grid, kRopeThreads, 0, stream>>>(a);
+      rope_kernel<append, fp8, true, norm><<<grid, kRopeThreads, 0, stream>>>(a);
     else
-      rope_kernel<append, fp8, false><<<grid, kRopeThreads, 0, stream>>>(a);
+      rope_kernel<append, fp8, false, norm><<<grid, kRopeThreads, 0, stream>>>(a);
+  };
+  auto run = [&](auto append, auto fp8) {
+    if (a.q_weight)
+      launch(append, fp8, std::true_type{});
+    else
+      launch(append, fp8, std::false_type{});
   };
   if (timer) (void)hipEventRecord(timer->start, stream);
   if (!a.slots)

@@ -78,6 +78,20 @@ def lib() -> ctypes.CDLL:
         L.rl_attn_rope.argtypes = [P, P, P, P, P, R, P, P, vp]
         L.rl_attn_rope_append_kv.argtypes = [P, P, P, P, P, P, R, P, P, P, P, P, vp]
         L.rl_attn_rope_append_kv_fp8.argtypes = [P, P, P, P, P, P, R, P, P, P, P, P, P, P, vp]
+        F = ctypes.c_float
+        L.rl_attn_norm_rope.argtypes = [P, P, P, P, F, P, P, P, R, P, P, vp]
+        L.rl_attn_norm_rope_append_kv.argtypes = [P, P, P, P, P, F, P, P, P, R, P, P, P, P, P, vp]
+        L.rl_attn_norm_rope_append_kv_fp8.argtypes = [P, P, P, P, P, F, P, P, P, R, P, P, P, P, P, P, P, vp]
+        L.rl_attn_norm_rope_backward.argtypes = [P, P, P, P, P, P, F, P, P, P, R, P, P, P, P, vp]
+        L.rl_attn_norm_rope_backward_workspace_size.argtypes = []
+        L.rl_attn_norm_rope_backward_workspace_size.restype = ctypes.c_size_t
+        L.rl_attn_token_logprobs.argtypes = [P] * 8 + [vp]
+        L.rl_attn_token_logprobs_backward.argtypes = [P] * 8 + [vp]
+        L.rl_attn_token_logprobs_workspace_size.argtypes = [ctypes.c_int64] * 3
+        L.rl_attn_token_logprobs_workspace_size.restype = ctypes.c_size_t
+        L.rl_attn_fork_requests.argtypes = [P, P, P, P, P, ctypes.c_int64, ctypes.c_int64, P, P, P, P, vp]
+        L.rl_attn_copy_pages.argtypes = [P, P, P, vp]
+        L.rl_attn_drop_tokens.argtypes = [P, P, P, ctypes.c_int64, ctypes.c_int64, P, P, P, P, vp]
         L.rl_attn_prefill.argtypes = [P, P, P, P, ctypes.c_float, P, P, vp]
         L.rl_attn_merge.argtypes = [P, P, P, P, P, vp]
         L.rl_attn_last_error.restype = ctypes.c_char_p
@@ -101,6 +115,9 @@ def lib() -> ctypes.CDLL:
                      "rl_attn_decode_noalloc",
                      "rl_attn_decode_fp8", "rl_attn_extend_fp8", "rl_attn_append_kv", "rl_attn_append_kv_fp8",
                      "rl_attn_map_slots", "rl_attn_rope", "rl_attn_rope_append_kv", "rl_attn_rope_append_kv_fp8",
+                     "rl_attn_norm_rope", "rl_attn_norm_rope_append_kv", "rl_attn_norm_rope_append_kv_fp8",
+                     "rl_attn_norm_rope_backward", "rl_attn_token_logprobs", "rl_attn_token_logprobs_backward",
+                     "rl_attn_fork_requests", "rl_attn_copy_pages", "rl_attn_drop_tokens",
                      "rl_attn_prefill", "rl_attn_merge", "rl_attn_check_device_errors", "rl_attn_reserve_workspace",
                      "rl_attn_profile_enable", "rl_attn_profile_read", "rl_attn_diag_read_bandwidth",
                      "rl_attn_diag_mfma_bf16", "rl_attn_diag_decode_capacity", "rl_attn_diag_extend_capacity",
@@ -366,6 +383,167 @@ def rope_append_kv_fp8(q, k_new, v_new, positions, inv_freq, slot_map, k_pages, 
                                             _arg(k_out), _arg(k_pages), _arg(v_pages), _arg(k_scale),
                                             _arg(v_scale), _stream(stream)))
     return q_out
+
+
+def norm_rope(q, k, q_weight, k_weight, eps, positions, inv_freq, axes=None, *, interleaved=False, q_out=None,
+              k_out=None, stream=None):
+    """``rl_attn_norm_rope``: returns ``(q_out, k_out)`` (``k`` and ``k_weight`` may be None)."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None and k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    _check(lib().rl_attn_norm_rope(_arg(q), _arg(k), _arg(q_weight), _arg(k_weight), eps, _arg(positions),
+                                   _arg(inv_freq), _arg(axes), _rope_opts(interleaved), _arg(q_out), _arg(k_out),
+                                   _stream(stream)))
+    return q_out, k_out
+
+
+def norm_rope_append_kv(q, k_new, v_new, q_weight, k_weight, eps, positions, inv_freq, slot_map, k_pages, v_pages,
+                        axes=None, *, interleaved=False, q_out=None, k_out=None, stream=None):
+    """``rl_attn_norm_rope_append_kv``: returns ``q_out``; ``k_out`` (rows of keys) is written only if given."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(lib().rl_attn_norm_rope_append_kv(_arg(q), _arg(k_new), _arg(v_new), _arg(q_weight), _arg(k_weight), eps,
+                                             _arg(positions), _arg(inv_freq), _arg(axes), _rope_opts(interleaved),
+                                             _arg(slot_map), _arg(q_out), _arg(k_out), _arg(k_pages), _arg(v_pages),
+                                             _stream(stream)))
+    return q_out
+
+
+def norm_rope_append_kv_fp8(q, k_new, v_new, q_weight, k_weight, eps, positions, inv_freq, slot_map, k_pages, v_pages,
+                            k_scale, v_scale, axes=None, *, interleaved=False, q_out=None, k_out=None, stream=None):
+    """``rl_attn_norm_rope_append_kv_fp8``: as ``norm_rope_append_kv`` into ``torch.float8_e4m3fn`` pages."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(lib().rl_attn_norm_rope_append_kv_fp8(
+        _arg(q), _arg(k_new), _arg(v_new), _arg(q_weight), _arg(k_weight), eps, _arg(positions), _arg(inv_freq),
+        _arg(axes), _rope_opts(interleaved), _arg(slot_map), _arg(q_out), _arg(k_out), _arg(k_pages), _arg(v_pages),
+        _arg(k_scale), _arg(v_scale), _stream(stream)))
+    return q_out
+
+
+class NormRopeGrads(NamedTuple):
+    """What ``norm_rope_backward`` gives (None for k where there is none)."""
+
+    dq: torch.Tensor
+    dk: Optional[torch.Tensor]
+    dq_weight: torch.Tensor
+    dk_weight: Optional[torch.Tensor]
+
+
+def norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, eps, positions, inv_freq, axes=None, *,
+                       interleaved=False, dq=None, dk=None, dq_weight=None, dk_weight=None,
+                       stream=None) -> NormRopeGrads:
+    """``rl_attn_norm_rope_backward``: gradients of ``norm_rope``. ``dq=dq_out, dk=dk_out`` works in place."""
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if dq_weight is None:
+        dq_weight = torch.empty(q_weight.shape, dtype=torch.float32, device=q.device)
+    if k is not None:
+        if dk is None:
+            dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        if dk_weight is None:
+            dk_weight = torch.empty(k_weight.shape, dtype=torch.float32, device=k.device)
+    _check(lib().rl_attn_norm_rope_backward(_arg(dq_out), _arg(dk_out), _arg(q), _arg(k), _arg(q_weight),
+                                            _arg(k_weight), eps, _arg(positions), _arg(inv_freq), _arg(axes),
+                                            _rope_opts(interleaved), _arg(dq), _arg(dk), _arg(dq_weight),
+                                            _arg(dk_weight), _stream(stream)))
+    return NormRopeGrads(dq, dk, dq_weight, dk_weight)
+
+
+def norm_rope_backward_workspace_size() -> int:
+    return int(lib().rl_attn_norm_rope_backward_workspace_size())
+
+
+class TokenLogprobs(NamedTuple):
+    """What ``token_logprobs`` gives (None for alternatives that were not asked for)."""
+
+    logprobs: torch.Tensor
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_ids: Optional[torch.Tensor]
+    top_logprobs: Optional[torch.Tensor]
+
+
+def token_logprobs(logits, tokens, row_scale=None, *, top=0, logprobs=None, entropy=None, lse=None, top_ids=None,
+                   top_logprobs=None, stream=None) -> TokenLogprobs:
+    """``rl_attn_token_logprobs``: ``top`` is the number of alternatives where ``top_ids`` is not given."""
+    rows, dev = logits.shape[0], logits.device
+    if logprobs is None:
+        logprobs = torch.empty(rows, dtype=torch.float32, device=dev)
+    if entropy is None:
+        entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    if lse is None:
+        lse = torch.empty(rows, dtype=torch.float32, device=dev)
+    if top_ids is not None:
+        top = top_ids.shape[-1]
+    elif top_logprobs is not None:
+        top = top_logprobs.shape[-1]
+    if top_ids is None and top:
+        top_ids = torch.empty((rows, top), dtype=torch.int32, device=dev)
+    if top_logprobs is None and top_ids is not None:
+        top_logprobs = torch.empty((rows, top), dtype=torch.float32, device=dev)
+    _check(lib().rl_attn_token_logprobs(_arg(logits), _arg(tokens), _arg(row_scale), _arg(logprobs), _arg(entropy),
+                                        _arg(lse), _arg(top_ids), _arg(top_logprobs), _stream(stream)))
+    return TokenLogprobs(logprobs, entropy, lse, top_ids, top_logprobs)
+
+
+def token_logprobs_backward(logits, tokens, lse, d_logprobs, row_scale=None, *, entropy=None, d_entropy=None,
+                            d_logits=None, stream=None):
+    """``rl_attn_token_logprobs_backward``: returns ``d_logits`` (``d_logits=logits`` works in place)."""
+    if d_logits is None:
+        d_logits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _check(lib().rl_attn_token_logprobs_backward(_arg(logits), _arg(tokens), _arg(row_scale), _arg(lse), _arg(entropy),
+                                                 _arg(d_logprobs), _arg(d_entropy), _arg(d_logits),
+                                                 _stream(stream)))
+    return d_logits
+
+
+def token_logprobs_workspace_size(rows: int, vocab: int, top: int = 0) -> int:
+    return int(lib().rl_attn_token_logprobs_workspace_size(rows, vocab, top))
+
+
+class Forked(NamedTuple):
+    """What ``fork_requests`` gives (the block table is written in place)."""
+
+    kv_lens: torch.Tensor
+    free_used: torch.Tensor
+    copies: torch.Tensor
+
+
+def fork_requests(parents, fork_lens, kv_lens, free_pages, free_used, block_table, page_size, num_pages, *,
+                  kv_lens_out=None, free_used_out=None, copies=None, stream=None) -> Forked:
+    """``rl_attn_fork_requests``. ``kv_lens_out=kv_lens, free_used_out=free_used`` works in place."""
+    if kv_lens_out is None:
+        kv_lens_out = torch.empty_like(kv_lens)
+    if free_used_out is None:
+        free_used_out = torch.empty_like(free_used)
+    if copies is None:
+        copies = torch.empty((kv_lens.shape[0], 3), dtype=torch.int32, device=kv_lens.device)
+    _check(lib().rl_attn_fork_requests(_arg(parents), _arg(fork_lens), _arg(kv_lens), _arg(free_pages),
+                                       _arg(free_used), page_size, num_pages, _arg(block_table), _arg(kv_lens_out),
+                                       _arg(free_used_out), _arg(copies), _stream(stream)))
+    return Forked(kv_lens_out, free_used_out, copies)
+
+
+def copy_pages(copies, k_pages, v_pages, *, stream=None):
+    """``rl_attn_copy_pages``: the rows that a fork copies, in one layer's pages (in place)."""
+    _check(lib().rl_attn_copy_pages(_arg(copies), _arg(k_pages), _arg(v_pages), _stream(stream)))
+
+
+def drop_tokens(kv_lens, keep_lens, block_table, free_pages, free_used, page_size, num_pages, *, kv_lens_out=None,
+                free_used_out=None, stream=None):
+    """``rl_attn_drop_tokens``: writes ``free_pages``, returns ``(kv_lens_out, free_used_out)``.
+
+    ``kv_lens_out=kv_lens, free_used_out=free_used`` works in place."""
+    if kv_lens_out is None:
+        kv_lens_out = torch.empty_like(kv_lens)
+    if free_used_out is None:
+        free_used_out = torch.empty_like(free_used)
+    _check(lib().rl_attn_drop_tokens(_arg(kv_lens), _arg(keep_lens), _arg(block_table), page_size, num_pages,
+                                     _arg(free_pages), _arg(free_used), _arg(kv_lens_out), _arg(free_used_out),
+                                     _stream(stream)))
+    return kv_lens_out, free_used_out
 
 
 def prefill(q, k, v, seq_indptr, scale, out=None, lse=None, *, stream=None):

@@ -1,0 +1,295 @@
+"""Requests that fork and drop their tokens on the GPU (through the C-ABI): whole numbers and copies, equal to their
+definition."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ends
+from paper_2609_08368_amd import rl_attn as ra
+from tests import gpu_helpers as H
+from tests.test_gpu_step import dev, rand
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def errors_reported():
+    try:
+        ra.check_device_errors()
+    except ra.RlAttnError as e:
+        return set(str(e).split("):")[1].split())
+    return set()
+
+
+def fork_case(seed, batch, hi, page, share=0.5, used=4):
+    rng = np.random.default_rng(seed)
+    forked = rng.random(batch) < share
+    forked[int(rng.integers(batch))] = False
+    lens = np.where(forked, 0, rng.integers(0, hi + 1, batch))
+    parents = np.where(forked, rng.choice(np.flatnonzero(~forked), batch), -1 - rng.integers(0, 5, batch))
+    want = np.where(forked, np.minimum(lens[np.maximum(parents, 0)], rng.integers(0, hi + 1, batch)), -3)
+    whole = rng.random(batch) < 0.4
+    want = np.where(forked & whole, lens[np.maximum(parents, 0)], want)
+    held = -(-lens // page)
+    pool = int(held.sum()) + batch + 9
+    ids = rng.permutation(pool)
+    table = np.full((batch, int(held.max()) + 2), -5)
+    table[np.arange(table.shape[1])[None] < held[:, None]] = ids[:int(held.sum())]
+    free = np.concatenate([rng.integers(0, pool, used), ids[int(held.sum()):]])
+    return dict(parents=parents, fork_lens=want, kv_lens=lens, free_pages=free, free_used=used, block_table=table,
+                page_size=page, num_pages=pool)
+
+
+def run_fork(c, in_place=False):
+    t = {k: dev(c[k]) for k in ("parents", "fork_lens", "kv_lens", "free_pages", "block_table")}
+    used = dev(np.array([c["free_used"]]))
+    more = dict(kv_lens_out=t["kv_lens"], free_used_out=used) if in_place else {}
+    f = ra.fork_requests(t["parents"], t["fork_lens"], t["kv_lens"], t["free_pages"], used, t["block_table"],
+                         c["page_size"], c["num_pages"], **more)
+    torch.cuda.synchronize()
+    return f, t
+
+
+def check_fork(c, in_place=False):
+    want = ends.fork_requests(**c)
+    f, t = run_fork(c, in_place)
+    assert np.array_equal(t["block_table"].cpu().numpy(), want["block_table"])
+    assert np.array_equal(f.kv_lens.cpu().numpy(), want["kv_lens"])
+    assert np.array_equal(f.copies.cpu().numpy(), want["copies"])
+    assert int(f.free_used) == want["free_used"]
+    if not in_place:
+        assert np.array_equal(t["kv_lens"].cpu().numpy(), c["kv_lens"])
+    assert errors_reported() == want["errors"]
+    return want
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("case", [(1, 300, 64), (2, 1, 8), (4, 128, 64), (5, 700, 16), (9, 16, 8), (144, 5000, 64),
+                                  (1023, 90, 8), (1025, 90, 16), (4096, 60, 16), (5001, 40, 8)], ids=str)
+def test_fork_equals_the_definition(case, in_place):
+    batch, hi, page = case
+    H.say(f"fork {case} in_place={in_place}")
+    for seed in range(3):
+        check_fork(fork_case(seed + batch, batch, hi, page), in_place)
+    check_fork(fork_case(batch, batch, 0, page), in_place)
+
+
+@pytest.mark.parametrize("change", [
+    lambda c: c["parents"].__setitem__(slice(None), np.arange(len(c["parents"]))),      # of themselves
+    lambda c: c["parents"].__setitem__(slice(None), 10 ** 6),
+    lambda c: c["parents"].__setitem__(slice(0, 20), 3),                                 # of one that may be forked
+    lambda c: c["kv_lens"].__setitem__(slice(5, 20), 1),
+    lambda c: c["kv_lens"].__setitem__(slice(5, 20), -1),
+    lambda c: c["kv_lens"].__setitem__(slice(5, 20), 10 ** 9),
+    lambda c: c["fork_lens"].__setitem__(slice(5, 20), -1),
+    lambda c: c["fork_lens"].__setitem__(slice(5, 20), 10 ** 9),
+    lambda c: c.update(free_pages=c["free_pages"][:9]), lambda c: c.update(free_pages=c["free_pages"][:0], free_used=0),
+    lambda c: c.update(free_used=10 ** 6), lambda c: c.update(free_used=-4),
+    lambda c: c["free_pages"].__setitem__(7, -1), lambda c: c["free_pages"].__setitem__(7, 10 ** 9),
+    lambda c: c["block_table"].__setitem__((slice(None), slice(0, 1)), -1)], ids=range(15))
+@pytest.mark.parametrize("size", [(40, 200, 16), (1500, 70, 8)], ids=str)
+def test_fork_refuses_and_reports(change, size):
+    c = fork_case(11, *size)
+    change(c)
+    for in_place in (False, True):
+        check_fork(c, in_place)
+
+
+def test_fork_takes_the_last_page_of_the_list():
+    c = fork_case(3, 30, 200, 16)
+    need = int((ends.fork_requests(**c)["copies"][:, 2] > 0).sum())
+    for n in (need - 1, need, need + 1):
+        want = check_fork({**c, "free_pages": c["free_pages"][:4 + n]})
+        assert bool(want["errors"]) == (n < need)
+
+
+def test_fork_of_nothing():
+    c = fork_case(3, 5, 50, 8)
+    for k in ("parents", "fork_lens", "kv_lens", "block_table"):
+        c[k] = c[k][:0]
+    check_fork(c)
+    check_fork(c, True)
+
+
+def test_fork_reads_strides():
+    c = fork_case(5, 20, 200, 16)
+    want = ends.fork_requests(**c)
+    wide = {k: dev(np.stack([c[k], c[k] * 0 - 8], 1)) for k in ("parents", "fork_lens", "kv_lens", "free_pages")}
+    table = dev(np.full((c["block_table"].shape[1], 2, 20), -5))
+    table[:, 1] = dev(c["block_table"]).T
+    lens, copies = (torch.full(s, -8, dtype=torch.int32, device=DEV) for s in ((20, 3), (20, 5)))
+    ra.fork_requests(wide["parents"][:, 0], wide["fork_lens"][:, 0], wide["kv_lens"][:, 0], wide["free_pages"][:, 0],
+                     dev(np.array([4])), table[:, 1].T, 16, c["num_pages"], kv_lens_out=lens[:, 1],
+                     copies=copies[:, 1:4])
+    assert np.array_equal(lens[:, 1].cpu().numpy(), want["kv_lens"]) and torch.all(lens[:, ::2] == -8)
+    assert np.array_equal(copies[:, 1:4].cpu().numpy(), want["copies"]) and torch.all(copies[:, ::4] == -8)
+    assert np.array_equal(table[:, 1].T.cpu().numpy(), want["block_table"]) and torch.all(table[:, 0] == -5)
+
+
+# -------------------------------------------------------------------------------------------------------- copies
+
+def pools(seed, pages, page, heads, fp8):
+    kind = torch.float8_e4m3fn if fp8 else torch.bfloat16
+    return [rand(seed + i, pages, page, heads, 128).to(kind) for i in (0, 1)]
+
+
+def raw(t):
+    return t.contiguous().view(torch.uint8).cpu().numpy()
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("case", [(1, 8, 1), (7, 16, 3), (40, 64, 8), (9, 128, 2), (300, 8, 1), (3, 64, 16)], ids=str)
+def test_copies_rows_of_pages(case, fp8):
+    n, page, heads = case
+    H.say(f"copy {case} fp8={fp8}")
+    rng = np.random.default_rng(n + page)
+    k, v = pools(n, 2 * n + 5, page, heads, fp8)
+    ids = rng.permutation(2 * n + 5)
+    copies = np.stack([rng.choice(ids[n:2 * n], n), ids[:n], rng.integers(-1, page + 1, n)], 1)   # one page for several
+    copies[0, 2] = page
+    want = [ends.copy_pages(copies, raw(x)) for x in (k, v)]
+    ra.copy_pages(dev(copies), k, v)
+    assert all(np.array_equal(raw(x), w) for x, w in zip((k, v), want))
+    ra.check_device_errors()
+
+
+def test_copies_in_pools_of_any_order():
+    k, v = pools(1, 12, 16, 3, False)
+    want = [ends.copy_pages([[1, 5, 9], [2, 6, 16]], raw(x)) for x in (k, v)]
+    k2 = k.permute(2, 0, 1, 3).contiguous().permute(1, 2, 0, 3)
+    both = torch.stack((v, v), dim=1)
+    ra.copy_pages(dev(np.array([[1, 5, 9, -1], [2, 6, 16, -1]]))[:, :3], k2, both[:, 1])
+    assert np.array_equal(raw(k2), want[0]) and np.array_equal(raw(both[:, 1]), want[1]) and torch.equal(both[:, 0], v)
+
+
+def test_copies_refuse_pages_that_are_not_there():
+    k, v = pools(2, 10, 16, 2, False)
+    before = [raw(x) for x in (k, v)]
+    for bad, what in (([-1, 3, 2], "page-id"), ([3, 10, 2], "page-id"), ([1 << 30, 3, 2], "page-id"),
+                      ([3, -(1 << 31), 1], "page-id"), ([3, 4, 17], "length"), ([3, 4, (1 << 31) - 1], "length")):
+        ra.copy_pages(dev(np.array([bad, [0, 1, 0], [5, 5, 16], [-1, -1, 0], [-1, -1, -5]])), k, v)
+        assert errors_reported() == {what + "-out-of-range"}
+        assert all(np.array_equal(raw(x), b) for x, b in zip((k, v), before))
+
+
+def test_copies_past_two_gigabytes():
+    """Pages whose offsets pass 32 bits."""
+    k = torch.zeros((40000, 64, 8, 128), dtype=torch.bfloat16, device=DEV)     # 5.2 GB
+    v = torch.zeros_like(k)
+    k[39990], v[39991] = rand(1, 64, 8, 128), rand(2, 64, 8, 128)
+    ra.copy_pages(dev(np.array([[39990, 3, 64], [39991, 39999, 33]])), k, v)
+    assert torch.equal(k[3], k[39990]) and torch.equal(v[39999, :33], v[39991, :33]) and torch.all(v[39999, 33:] == 0)
+    assert torch.all(k[2] == 0) and torch.all(k[4] == 0)
+
+
+# ---------------------------------------------------------------------------------------------------------- drops
+
+def drop_case(seed, batch, hi, page, shared=True, pool_extra=9, spread=1):
+    """Groups of up to four requests share the full pages of a prefix; ends, cuts, requests left as they are."""
+    rng = np.random.default_rng(seed)
+    lens = rng.integers(0, hi + 1, batch)
+    held = -(-lens // page)
+    table = np.full((batch, int(held.max()) + 2), -5)
+    room = int(held.sum()) + pool_extra
+    pool = room * spread
+    ids, at = rng.permutation(pool)[:room], 0
+    for b in range(batch):
+        first = 0
+        if shared and b % 4 and rng.random() < 0.8:
+            first = min(int(rng.integers(0, 1 + hi // page)), int(lens[b]) // page, int(lens[b - b % 4]) // page)
+            table[b, :first] = table[b - b % 4, :first]
+        n = int(held[b]) - first
+        table[b, first:held[b]] = ids[at:at + n]
+        at += n
+    what = rng.random(batch)
+    keep = np.where(what < 0.3, 0, np.where(what < 0.6, rng.integers(0, hi + 1, batch), 10 ** 9))
+    free = np.concatenate([rng.integers(0, pool, at + 3), ids[at:]])
+    return dict(kv_lens=lens, keep_lens=keep, block_table=table, free_pages=free, free_used=at + 3, page_size=page,
+                num_pages=pool)
+
+
+def check_drop(c, in_place=False):
+    want = ends.drop_tokens(**c)
+    t = {k: dev(c[k]) for k in ("kv_lens", "keep_lens", "free_pages", "block_table")}
+    used = dev(np.array([c["free_used"]]))
+    more = dict(kv_lens_out=t["kv_lens"], free_used_out=used) if in_place else {}
+    lens, left = ra.drop_tokens(t["kv_lens"], t["keep_lens"], t["block_table"], t["free_pages"], used, c["page_size"],
+                                c["num_pages"], **more)
+    torch.cuda.synchronize()
+    assert np.array_equal(lens.cpu().numpy(), want["kv_lens"])
+    assert int(left) == want["free_used"]
+    assert np.array_equal(t["free_pages"].cpu().numpy(), want["free_pages"])
+    assert np.array_equal(t["block_table"].cpu().numpy(), c["block_table"])
+    assert errors_reported() == want["errors"]
+    return want
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("case", [(1, 1, 8), (1, 300, 64), (7, 500, 16), (128, 9000, 64), (1023, 90, 8),
+                                  (3001, 400, 16), (64, 20000, 8)], ids=str)
+def test_drop_equals_the_definition(case, in_place):
+    batch, hi, page = case
+    H.say(f"drop {case} in_place={in_place}")
+    for seed in range(3):
+        check_drop(drop_case(seed + batch, batch, hi, page, shared=seed > 0), in_place)
+    c = drop_case(batch, batch, hi, page)
+    check_drop({**c, "keep_lens": c["kv_lens"]}, in_place)             # nothing ends
+    check_drop({**c, "keep_lens": c["kv_lens"] * 0}, in_place)         # everything does
+    check_drop({**c, "kv_lens": c["kv_lens"] * 0}, in_place)
+
+
+@pytest.mark.parametrize("spread", [300, 3000])
+def test_drop_in_large_pools(spread):
+    """Ids all over a pool of 334 thousand and of 3.3 million pages."""
+    for in_place in (False, True):
+        c = drop_case(5, 60, 600, 16, spread=spread)
+        want = check_drop(c, in_place)
+        assert want["free_used"] < c["free_used"] and c["num_pages"] > 300_000
+
+
+@pytest.mark.parametrize("change", [
+    lambda c: c["kv_lens"].__setitem__(slice(2, 9), -1), lambda c: c["kv_lens"].__setitem__(slice(2, 9), 10 ** 9),
+    lambda c: c["kv_lens"].__setitem__(2, 2 ** 31 - 1),
+    lambda c: c["keep_lens"].__setitem__(slice(2, 9), -1), lambda c: c["block_table"].__setitem__((3, 0), -1),
+    lambda c: c["block_table"].__setitem__((slice(None), 0), 10 ** 9),
+    lambda c: c.update(free_used=3), lambda c: c.update(free_used=-1), lambda c: c.update(free_used=0),
+    lambda c: c.update(free_used=10 ** 9), lambda c: c.update(num_pages=c["num_pages"] // 2),
+    lambda c: c.update(num_pages=0)], ids=range(12))
+@pytest.mark.parametrize("size", [(40, 200, 16), (1500, 70, 8)], ids=str)
+def test_drop_refuses_and_reports(change, size):
+    c = drop_case(11, *size)
+    change(c)
+    for in_place in (False, True):
+        check_drop(c, in_place)
+
+
+def test_drop_frees_a_page_once_and_keeps_what_others_hold():
+    """Eight attempts of a prompt end one after the other; the prompt goes with its last holder."""
+    table = np.full((9, 6), -1)
+    table[:, :3] = [7, 3, 5]
+    table[:, 3] = np.arange(10, 19)
+    lens, used, free = np.full(9, 60), 20, np.arange(30, 60)
+    for b in range(9):
+        keep = np.where(np.arange(9) == b, 0, 10 ** 9)
+        c = dict(kv_lens=lens, keep_lens=keep, block_table=table, free_pages=free, free_used=used, page_size=16,
+                 num_pages=60)
+        want = check_drop(c)
+        assert c["free_used"] - want["free_used"] == (4 if b == 8 else 1)
+        lens, used, free = want["kv_lens"], want["free_used"], want["free_pages"]
+    assert list(free[used:20]) == [3, 5, 7, 18, 17, 16, 15, 14, 13, 12, 11, 10]
+
+
+def test_drop_reads_strides_and_nothing():
+    c = drop_case(5, 20, 200, 16)
+    want = ends.drop_tokens(**c)
+    wide = {k: dev(np.stack([c[k], c[k] * 0 - 8], 1)) for k in ("kv_lens", "keep_lens", "free_pages")}
+    table = dev(c["block_table"].T.copy()).T
+    lens = torch.full((20, 3), -8, dtype=torch.int32, device=DEV)
+    _, left = ra.drop_tokens(wide["kv_lens"][:, 0], wide["keep_lens"][:, 0], table, wide["free_pages"][:, 0],
+                             dev(np.array([c["free_used"]])), 16, c["num_pages"], kv_lens_out=lens[:, 1])
+    assert np.array_equal(wide["free_pages"][:, 0].cpu().numpy(), want["free_pages"])
+    assert torch.all(wide["free_pages"][:, 1] == -8) and torch.all(lens[:, ::2] == -8)
+    assert np.array_equal(lens[:, 1].cpu().numpy(), want["kv_lens"]) and int(left) == want["free_used"]
+    none = {k: c[k][:0] if k in ("kv_lens", "keep_lens", "block_table") else c[k] for k in c}
+    check_drop(none)
