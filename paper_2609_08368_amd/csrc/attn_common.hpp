@@ -222,6 +222,34 @@ __device__ __forceinline__ uint64_t row_offset(uint32_t pg, uint32_t sp, int slo
   return (uint64_t)pg * sp + __umul24((uint32_t)slot, ss);
 }
 
+// Data that workgroups hand to the last of them to arrive: stored and loaded by
+// agent-scope atomics, which go through the L2s of the eight dies, so that no
+// workgroup has to write its whole L2 back (a release fence at agent scope in each of
+// 1400 workgroups took a 30 us kernel to 270). arrive() waits for the calling
+// wave's own stores and atomics, then for the workgroup's other waves, and counts; it
+// returns true in every thread of the last of n workgroups, which leaves the counter
+// at 0. All threads call it.
+template <typename T>
+__device__ __forceinline__ void hand_over(T* p, T v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ T handed_over(const T* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ bool arrive(int* counter, int n, int* last) {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    *last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == n;
+    if (*last) hand_over(counter, 0);
+  }
+  __syncthreads();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+  return *last;
+}
+
 // Inclusive prefix sums over a wave's 64 lanes, without LDS: DPP row shifts
 // (row_shr 1, 2, 4, 8; lanes shifted in from outside the 16-lane row read 0)
 // scan each row, then each row adds the totals of the rows below it, read from

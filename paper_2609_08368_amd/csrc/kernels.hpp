@@ -316,6 +316,7 @@ constexpr int kRopeGradGroupsPerCu = 4;             // at most
 // Log probabilities of tokens, and the gradient of their logits.
 constexpr int kLogprobSegment = 4096;               // logits a wave sums at once
 constexpr int kLogprobChunks = 16;                  // workgroups of a row, at most
+constexpr int kLogprobSharedRows = 2048;            // rows that several workgroups share, at most
 constexpr int kLogprobTop = 32;                     // alternatives, at most
 constexpr int kLogprobPartBytes = 12;               // of a segment's sums
 struct LogprobArgs {
@@ -342,7 +343,8 @@ struct LogprobArgs {
   int chunks;             // workgroups of a row
   int segs, segs_chunk;   // segments of a row and of a workgroup
   void* parts;            // chunks > 1: [rows, segs] sums
-  uint64_t* cands;   // chunks > 1: [rows, chunks, top] ranked tokens
+  uint64_t* cands;        // chunks > 1: [rows, chunks, top] ranked tokens
+  int* arrived;           // chunks > 1: [rows] workgroups that are through, 0 between calls
   int* err;
 };
 
@@ -378,6 +380,9 @@ struct CopyArgs {
 };
 
 // Requests that end or are cut back.
+constexpr int kDropPart = 7680 * 32;                // pages that a workgroup marks at once (two marks each: 60 KB)
+constexpr int kDropGroups = 16;                     // workgroups of a call, at most
+constexpr int kDropMarkBytes = 1 << 18;             // of the marks that they hand over
 struct DropArgs {
   const int* kv_lens;     // [B]
   const int* keep_lens;   // [B]
@@ -390,6 +395,8 @@ struct DropArgs {
   int* used_out;          // (may be free_used)
   int64_t kv_out_s;
   int B, n_free, num_pages, page_size, log2_page, max_pages;
+  int* arrived;           // workgroups that are through, 0 between calls
+  uint64_t* marks;        // kDropMarkBytes
   int* err;
 };
 

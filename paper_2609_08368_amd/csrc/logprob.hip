@@ -108,28 +108,38 @@ __device__ __forceinline__ RowInput read_row(const LogprobArgs& a, int64_t r, in
   return in;
 }
 
-// One segment's maximum and sums.
+// One segment's maximum and sums. y is taken around base(m) instead of m c (c = s
+// log2 e): a whole number where that is near, so that y = x c - base is one fused
+// product, rounded once; c itself is rounded, but the same for all logits of the row.
 struct Part {
   float m, s, y;
 };
+constexpr float kNear = 1048576.f;
+// m c - base(m)
+__device__ __forceinline__ float above_base(float m, float c) {
+  const float z = m * c;
+  return fabsf(z) <= kNear ? fmaf(m, c, -__builtin_rintf(z)) : 0.f;
+}
 
-// A wave's segment of n logits at x; *lane_max is the largest of this lane's.
+// Loads of a lane for a segment.
 template <typename X>
-__device__ __forceinline__ Part segment_part(const X* x, int n, float c, float* lane_max) {
-  constexpr int kLoads = kSegment / 64 / kPer<X>;
+constexpr int kLoads = kSegment / 64 / kPer<X>;
+
+// A wave's segment of n logits at x, left in w; *lane_max is the largest of this lane's.
+template <typename X>
+__device__ __forceinline__ Part segment_part(const X* x, int n, float c, u32x4 (&w)[kLoads<X>], float* lane_max) {
   const int at = (threadIdx.x & 63) * kPer<X>;
-  u32x4 w[kLoads];
   if (n == kSegment) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
+    for (int i = 0; i < kLoads<X>; ++i)
       w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(x + at + i * 64 * kPer<X>));
   } else {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) w[i] = load_logits(x, at + i * 64 * kPer<X>, n);
+    for (int i = 0; i < kLoads<X>; ++i) w[i] = load_logits(x, at + i * 64 * kPer<X>, n);
   }
   float top = kNegInf;
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
+  for (int i = 0; i < kLoads<X>; ++i) {
     float f[kPer<X>];
     unpack<X>(w[i], f);
 #pragma unroll
@@ -138,31 +148,51 @@ __device__ __forceinline__ Part segment_part(const X* x, int n, float c, float* 
   *lane_max = top;
   Part p{wave_max(top), 0.f, 0.f};
   const float m = p.m == kNegInf ? 0.f : p.m;       // (excluded tokens alone: every term is 0)
+  const float z = m * c;
+  auto sums = [&](auto y_of) {
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    float f[kPer<X>];
-    unpack<X>(w[i], f);
+    for (int i = 0; i < kLoads<X>; ++i) {
+      float f[kPer<X>];
+      unpack<X>(w[i], f);
 #pragma unroll
-    for (int e = 0; e < kPer<X>; ++e) {
-      const float y = (f[e] - m) * c, t = exp2_fast(y);
-      p.s += t;
-      p.y = fmaf(t, fmaxf(y, -1000.f), p.y);        // (0 times -inf)
+      for (int e = 0; e < kPer<X>; ++e) {
+        const float y = y_of(f[e]), t = exp2_fast(y);
+        p.s += t;
+        p.y = fmaf(t, fmaxf(y, -1000.f), p.y);      // (0 times -inf)
+      }
     }
+  };
+  if (fabsf(z) <= kNear) {
+    const float base = -__builtin_rintf(z);
+    sums([&](float v) { return fmaf(v, c, base); });
+  } else {
+    sums([&](float v) { return (v - m) * c; });     // (a product may overflow)
   }
   p.s = wave_sum(p.s);
   p.y = wave_sum(p.y);
   return p;
 }
 
-// The row's sums from its segments' (a wave; every lane receives them).
+// The row's sums from its segments' (a wave; every lane receives them). kShared: they
+// were handed over by several workgroups.
+template <bool kShared>
 __device__ __forceinline__ Part fold_parts(const Part* parts, int n, float c) {
   const int lane = threadIdx.x & 63;
-  float m = kNegInf;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, parts[i].m);
+  auto at = [&](int i) {
+    if constexpr (!kShared) return parts[i];
+    return Part{handed_over(&parts[i].m), handed_over(&parts[i].s), handed_over(&parts[i].y)};
+  };
+  Part first{kNegInf, 0.f, 0.f};
+  if (lane < n) first = at(lane);                   // (mostly all there is)
+  float m = first.m;
+  for (int i = lane + 64; i < n; i += 64) m = fmaxf(m, at(i).m);
   Part row{wave_max(m), 0.f, 0.f};
+  const float r = above_base(row.m, c);
   for (int i = lane; i < n; i += 64) {
-    const Part p = parts[i];
-    const float d = p.m == kNegInf ? 0.f : fmaxf((p.m - row.m) * c, -1000.f), f = exp2_fast(d);
+    const Part p = i == lane ? first : at(i);
+    // between the bases
+    const float d = p.m == kNegInf ? 0.f : fmaxf(fmaf(p.m - row.m, c, r - above_base(p.m, c)), -1000.f);
+    const float f = exp2_fast(d);
     row.s = fmaf(f, p.s, row.s);
     row.y = fmaf(f, fmaf(d, p.s, p.y), row.y);
   }
@@ -171,25 +201,26 @@ __device__ __forceinline__ Part fold_parts(const Part* parts, int n, float c) {
   return row;
 }
 
-// What a row answers with, from its sums.
+// What a row answers with, from its sums: log probabilities are (x - m) scale + rest.
 struct RowStats {
-  float m, log2s;
+  float m, rest;
   bool none;                                        // every token is excluded
 };
 __device__ __forceinline__ float log_prob(const RowStats& r, float x, float scale) {
-  return r.none ? kNegInf : (x - r.m) * scale - kLn2 * r.log2s;
+  return r.none ? kNegInf : fmaf(x - r.m, scale, r.rest);
 }
 
-template <typename X>
-__device__ __forceinline__ RowStats write_row(const LogprobArgs& a, int64_t r, const RowInput& in, const Part& p) {
+// x: the token's logit.
+__device__ __forceinline__ RowStats write_row(const LogprobArgs& a, int64_t r, float x, float scale, float c,
+                                              const Part& p) {
+  const float log2s = __builtin_amdgcn_logf(p.s);
   // (bits, not comparisons: the device code is compiled as if there were no NaN)
-  const RowStats st{p.m, __builtin_amdgcn_logf(p.s), (__float_as_uint(p.s) << 1) == 0};
+  const RowStats st{p.m, kLn2 * (above_base(p.m, c) - log2s), (__float_as_uint(p.s) << 1) == 0};
   if ((threadIdx.x & 63) == 0) {
-    const float x = (float)(static_cast<const X*>(a.x)[r * a.x_s + in.token]);
-    a.logprobs[r * a.lp_s] = log_prob(st, x, in.scale);
-    if (a.lse) a.lse[r * a.lse_s] = st.none ? kNegInf : fmaf(p.m, in.scale, kLn2 * st.log2s);
+    a.logprobs[r * a.lp_s] = log_prob(st, x, scale);
+    if (a.lse) a.lse[r * a.lse_s] = st.none ? kNegInf : fmaf(p.m, scale, -st.rest);
     if (a.entropy) {
-      float h = kLn2 * (st.log2s - p.y / p.s);
+      float h = kLn2 * (log2s - p.y / p.s);
       const uint32_t u = __float_as_uint(h);
       if (st.none || (u >= 0x80000000u && u <= 0xff800000u)) h = 0.f;     // (a rounding below 0)
       a.entropy[r * a.ent_s] = h;
@@ -213,7 +244,7 @@ __device__ __forceinline__ void write_masked(const LogprobArgs& a, int64_t r) {
 }
 
 struct TopLds {
-  uint32_t keys[kLpThreads];
+  __attribute__((aligned(16))) uint32_t keys[kLpThreads];
   uint64_t cand[kCand];
   uint64_t best[kLogprobTop];
   uint32_t tau;
@@ -221,84 +252,125 @@ struct TopLds {
   int n_winners, n_cand;
 };
 
-// The `top` largest of t.cand[0 .. n) to t.best, in order; 0 behind the last.
+// The `top` largest of t.cand[0 .. n) to t.best, in order; 0 behind the last. (Each
+// counts the larger ones; reads of a fixed number at a time overlap.)
 __device__ __forceinline__ void rank_candidates(TopLds& t, int n, int top) {
   const int tid = threadIdx.x;
+  const int padded = (n + 7) & ~7;                  // (kCand is a multiple of 8)
   if (tid < top) t.best[tid] = 0;
+  if (tid < padded - n) t.cand[n + tid] = 0;
   __syncthreads();
   for (int i = tid; i < n; i += kLpThreads) {
     const uint64_t mine = t.cand[i];
     int rank = 0;
-    for (int j = 0; j < n && rank < top; ++j) rank += t.cand[j] > mine;
+    for (int j = 0; j < padded; j += 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) rank += t.cand[j + k] > mine;
+    }
     if (mine != 0 && rank < top) t.best[rank] = mine;
   }
   __syncthreads();
 }
 
+// A bound that at least `top` of the workgroup's threads' largest logits reach, and
+// hardly more: bit by bit from the top, until the count is near enough.
+__device__ __forceinline__ void find_bound(TopLds& t, float lane_max, int top) {
+  constexpr int kSlack = 8;                         // (a few more to look at cost less than more bits)
+  const int tid = threadIdx.x;
+  t.keys[tid] = key_of(lane_max);
+  __syncthreads();
+  if (tid < 64) {
+    const u32x4 k = *reinterpret_cast<const u32x4*>(&t.keys[4 * tid]);
+    uint32_t lo = 0;
+    for (uint32_t bit = 0x80000000u; bit != 0; bit >>= 1) {
+      const uint32_t next = lo | bit;
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(k[i] >= next));
+      if (n < top) continue;
+      lo = next;
+      if (n <= top + kSlack) break;
+    }
+    if (tid == 0) {
+      t.tau = max(lo, kKeyNegInf + 1);              // excluded tokens are no alternatives
+      t.n_winners = t.n_cand = 0;
+    }
+  }
+  __syncthreads();
+}
+
+// Those of sixteen bytes of logits from element e on that reach the bound, to the list.
+template <typename X>
+__device__ __forceinline__ void add_candidates(TopLds& t, u32x4 w, int e, uint32_t tau) {
+  const float bound = float_of(tau);
+  float f[kPer<X>];
+  unpack<X>(w, f);
+#pragma unroll
+  for (int j = 0; j < kPer<X>; ++j) {
+    if (!(f[j] >= bound)) continue;                 // (cheaper than its key; NaN may pass, and its key does not)
+    const uint32_t k = key_of(f[j]);
+    if (k < tau) continue;
+    const int at = atomicAdd(&t.n_cand, 1);
+    if (at < kCand) t.cand[at] = rank_of(k, e + j);
+  }
+}
+
 // The workgroup's likeliest tokens to t.best: of segments seg0 .. seg1-1 of row x,
 // where wave w has seg0 + w, seg0 + w + kLpWaves, ... and lane_max is this
-// thread's largest logit of those.
-template <typename X>
-__device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int seg0, int seg1, float lane_max, int top) {
-  constexpr int kLoads = kSegment / 64 / kPer<X>;
+// thread's largest logit of those. kHeld: each wave has one, which is in w.
+template <typename X, bool kHeld>
+__device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int seg0, int seg1, float lane_max,
+                                         const u32x4 (&w)[kLoads<X>], int top) {
   const int tid = threadIdx.x;
-  const uint32_t key = key_of(lane_max);
-  t.keys[tid] = key;
-  if (tid == 0) t.n_winners = t.n_cand = 0;
-  __syncthreads();
-  int rank = 0;
-#pragma unroll 4
-  for (int j = 0; j < kLpThreads; ++j) rank += t.keys[j] > key || (t.keys[j] == key && j < tid);
-  if (rank == top - 1) t.tau = key;
-  __syncthreads();
-  const uint32_t tau = max(t.tau, kKeyNegInf + 1);  // excluded tokens are no alternatives
-  if (key >= tau) t.winners[atomicAdd(&t.n_winners, 1)] = tid;
-  __syncthreads();
-  const int rounds = (seg1 - seg0 + kLpWaves - 1) / kLpWaves, per = rounds * kLoads, n = t.n_winners * per;
-  for (int p = tid; p < n; p += kLpThreads) {
-    const int who = t.winners[p / per], i = p % per;
-    const int seg = seg0 + (who >> 6) + (i / kLoads) * kLpWaves;
-    const int e = seg * kSegment + ((i % kLoads) * 64 + (who & 63)) * kPer<X>;
-    if (seg >= seg1 || e >= vocab) continue;
-    float f[kPer<X>];
-    unpack<X>(load_logits(x, e, vocab), f);
+  find_bound(t, lane_max, top);
+  const uint32_t tau = t.tau;
+  const bool wins = key_of(lane_max) >= tau;
+  if constexpr (kHeld) {
+    if (wins) {
+      const int e = (seg0 + (tid >> 6)) * kSegment + (tid & 63) * kPer<X>;
 #pragma unroll
-    for (int j = 0; j < kPer<X>; ++j) {
-      const uint32_t k = key_of(f[j]);
-      if (k < tau) continue;
-      const int at = atomicAdd(&t.n_cand, 1);
-      if (at < kCand) t.cand[at] = rank_of(k, e + j);
+      for (int i = 0; i < kLoads<X>; ++i) add_candidates<X>(t, w[i], e + i * 64 * kPer<X>, tau);
+    }
+  } else {
+    if (wins) t.winners[atomicAdd(&t.n_winners, 1)] = tid;
+    __syncthreads();
+    const int rounds = (seg1 - seg0 + kLpWaves - 1) / kLpWaves, per = rounds * kLoads<X>, n = t.n_winners * per;
+    for (int p = tid; p < n; p += kLpThreads) {
+      const int who = t.winners[p / per], i = p % per;
+      const int seg = seg0 + (who >> 6) + (i / kLoads<X>) * kLpWaves;
+      const int e = seg * kSegment + ((i % kLoads<X>) * 64 + (who & 63)) * kPer<X>;
+      if (seg < seg1 && e < vocab) add_candidates<X>(t, load_logits(x, e, vocab), e, tau);
     }
   }
   __syncthreads();
   int found = t.n_cand;
-  if (found > kCand) {
-    // so many equal logits that the list does not hold them: one after the other,
-    // each the largest below the last
-    const int lo = seg0 * kSegment, hi = min(vocab, seg1 * kSegment);
-    uint64_t below = ~0ull;
-    for (found = 0; found < top; ++found) {
-      uint64_t most = 0;
-      for (int e = lo + tid; e < hi; e += kLpThreads) {
-        const uint64_t v = rank_of(key_of((float)x[e]), e);
-        if (v < below && v > most) most = v;
-      }
-      __syncthreads();                              // (the last round's list has been read)
-      t.cand[tid] = most;
-      __syncthreads();
-      for (int s = kLpThreads / 2; s > 0; s >>= 1) {
-        if (tid < s && t.cand[tid + s] > t.cand[tid]) t.cand[tid] = t.cand[tid + s];
-        __syncthreads();
-      }
-      below = t.cand[0];
-      if ((uint32_t)(below >> 32) <= kKeyNegInf) break;
-      if (tid == 0) t.best[found] = below;
-    }
-    if (tid < top && tid >= found) t.best[tid] = 0;
-    __syncthreads();
+  if (found <= kCand) {
+    rank_candidates(t, found, top);
     return;
   }
-  rank_candidates(t, found, top);
+  // so many equal logits that the list does not hold them: one after the other,
+  // each the largest below the last
+  const int lo = seg0 * kSegment, hi = min(vocab, seg1 * kSegment);
+  uint64_t below = ~0ull;
+  for (found = 0; found < top; ++found) {
+    uint64_t most = 0;
+    for (int e = lo + tid; e < hi; e += kLpThreads) {
+      const uint64_t v = rank_of(key_of((float)x[e]), e);
+      if (v < below && v > most) most = v;
+    }
+    __syncthreads();                                // (the last round's list has been read)
+    t.cand[tid] = most;
+    __syncthreads();
+    for (int s = kLpThreads / 2; s > 0; s >>= 1) {
+      if (tid < s && t.cand[tid + s] > t.cand[tid]) t.cand[tid] = t.cand[tid + s];
+      __syncthreads();
+    }
+    below = t.cand[0];
+    if ((uint32_t)(below >> 32) <= kKeyNegInf) break;
+    if (tid == 0) t.best[found] = below;
+  }
+  if (tid < top && tid >= found) t.best[tid] = 0;
+  __syncthreads();
 }
 
 // t.best as the row's alternatives.
@@ -311,68 +383,69 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, int64_t r, const
   a.top_lps[r * a.tl_s + i] = b ? log_prob(st, float_of((uint32_t)(b >> 32)), scale) : kNegInf;
 }
 
-// Workgroup: segments of one row. Where a row is one workgroup's, that answers;
-// otherwise the segments' sums and the workgroup's likeliest tokens go to memory.
-template <typename X, bool kTop>
+// Workgroup: segments of one row. Where a row is shared, its workgroups leave the
+// segments' sums and their likeliest tokens in memory, and the last of them to
+// arrive answers. kHeld: a wave has one segment at most.
+template <typename X, bool kTop, bool kHeld>
 __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobArgs a) {
-  extern __shared__ Part parts[];                   // [segs_chunk]
+  extern __shared__ Part parts[];                   // a workgroup for each row: [segs]
   __shared__ TopLds top;
+  __shared__ int last;
   const int row32 = blockIdx.x / a.chunks, chunk = blockIdx.x - row32 * a.chunks;
   const int64_t r = row32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int bad = 0;
   const RowInput in = read_row(a, r, &bad);
   if (in.token < 0) {
     if (chunk != 0) return;
-    if (bad && threadIdx.x == 0) atomicOr(a.err, bad);
+    if (bad && tid == 0) atomicOr(a.err, bad);
     write_masked(a, r);
     return;
   }
   const X* x = static_cast<const X*>(a.x) + r * a.x_s;
-  const float c = in.scale * kLog2e;
+  const float c = in.scale * kLog2e, x_token = (float)x[in.token];
   const int seg0 = chunk * a.segs_chunk, seg1 = min(a.segs, seg0 + a.segs_chunk);
+  Part* shared = a.chunks > 1 ? static_cast<Part*>(a.parts) + r * a.segs : nullptr;
   float most = kNegInf;
+  u32x4 w[kLoads<X>];
   for (int s = seg0 + wave; s < seg1; s += kLpWaves) {
     float lane_max;
-    const Part p = segment_part(x + s * kSegment, min(kSegment, a.vocab - s * kSegment), c, &lane_max);
+    const Part p = segment_part(x + s * kSegment, min(kSegment, a.vocab - s * kSegment), c, w, &lane_max);
     most = fmaxf(most, lane_max);
-    if ((threadIdx.x & 63) == 0) {
-      if (a.chunks == 1)
+    if ((tid & 63) == 0) {
+      if (shared) {
+        hand_over(&shared[s].m, p.m);
+        hand_over(&shared[s].s, p.s);
+        hand_over(&shared[s].y, p.y);
+      } else {
         parts[s] = p;
-      else
-        reinterpret_cast<Part*>(a.parts)[r * a.segs + s] = p;
+      }
     }
+    if (kHeld) break;
   }
-  if constexpr (kTop) find_top(top, x, a.vocab, seg0, seg1, most, a.top);
-  if (a.chunks > 1) {
-    if (kTop && threadIdx.x < a.top) a.cands[(r * a.chunks + chunk) * a.top + threadIdx.x] = top.best[threadIdx.x];
-    return;
+  if constexpr (kTop) find_top<X, kHeld>(top, x, a.vocab, seg0, seg1, most, w, a.top);
+  Part sums;
+  if (shared) {
+    uint64_t* cands = a.cands + r * a.chunks * a.top;
+    if (kTop && tid < a.top) hand_over(cands + chunk * a.top + tid, top.best[tid]);
+    if (!arrive(a.arrived + r, a.chunks, &last)) return;
+    // (one wave folds the sums while the others fetch the tokens)
+    if (wave == 0) sums = fold_parts<true>(shared, a.segs, c);
+    if constexpr (kTop) {
+      const int n = a.chunks * a.top;
+      if (wave != 0)
+        for (int i = tid - 64; i < n; i += kLpThreads - 64) top.cand[i] = handed_over(cands + i);
+      __syncthreads();
+      rank_candidates(top, n, a.top);
+    }
+  } else {
+    __syncthreads();
+    if (wave == 0) sums = fold_parts<false>(parts, a.segs, c);
   }
-  __syncthreads();
   if (wave == 0) {
-    const RowStats st = write_row<X>(a, r, in, fold_parts(parts, a.segs, c));
+    const RowStats st = write_row(a, r, x_token, in.scale, c, sums);
     if (kTop) write_top(a, r, top, st, in.scale);
   }
-}
-
-// Workgroup: one row of several workgroups' parts.
-template <typename X, bool kTop>
-__global__ __launch_bounds__(kLpThreads) void logprob_join_kernel(LogprobArgs a) {
-  __shared__ TopLds top;
-  const int64_t r = blockIdx.x;
-  int bad = 0;
-  const RowInput in = read_row(a, r, &bad);
-  if (in.token < 0) return;                         // (written and reported by its first workgroup)
-  if constexpr (kTop) {
-    const int n = a.chunks * a.top;
-    for (int i = threadIdx.x; i < n; i += kLpThreads) top.cand[i] = a.cands[r * n + i];
-    __syncthreads();
-    rank_candidates(top, n, a.top);
-  }
-  if (threadIdx.x >= 64) return;
-  const Part p = fold_parts(reinterpret_cast<const Part*>(a.parts) + r * a.segs, a.segs, in.scale * kLog2e);
-  const RowStats st = write_row<X>(a, r, in, p);
-  if (kTop) write_top(a, r, top, st, in.scale);
 }
 
 // Gradient: d_x_j = s (g (delta_j - p_j) - h p_j (ln p_j + H)), an element-wise pass.
@@ -437,6 +510,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_grad_kernel(LogprobArgs a)
 // takes, of four segments at least.
 int logprob_chunks(int64_t rows, int vocab, int cus) {
   const int segs = (vocab + kSegment - 1) / kSegment;
+  if (rows > kLogprobSharedRows) return 1;
   const int64_t want = std::max<int64_t>(1, (8 * (int64_t)cus + rows - 1) / std::max<int64_t>(rows, 1));
   const int most = std::min(kLogprobChunks, (segs + kLpWaves - 1) / kLpWaves);
   const int chunks = (int)std::min<int64_t>(want, std::max(1, most));
@@ -450,15 +524,23 @@ hipError_t launch_logprob(const LogprobArgs& args, hipStream_t stream) {
   a.segs_chunk = ((a.segs + a.chunks - 1) / a.chunks + kLpWaves - 1) / kLpWaves * kLpWaves;
   const unsigned grid = (unsigned)((int64_t)a.rows * a.chunks);
   const size_t lds = a.chunks == 1 ? sizeof(Part) * (size_t)a.segs : 0;
-  auto run = [&](auto type, auto top) {
-    typedef decltype(type) X;
-    logprob_kernel<X, decltype(top)::value><<<grid, kLpThreads, lds, stream>>>(a);
-    if (a.chunks > 1) logprob_join_kernel<X, decltype(top)::value><<<(unsigned)a.rows, kLpThreads, 0, stream>>>(a);
+  auto run = [&](auto type, auto top, auto held) {
+    logprob_kernel<decltype(type), decltype(top)::value, decltype(held)::value>
+        <<<grid, kLpThreads, lds, stream>>>(a);
+  };
+  auto run_type = [&](auto type) {
+    const bool held = a.segs_chunk <= kLpWaves;
+    if (!a.top)
+      run(type, std::false_type{}, std::false_type{});
+    else if (held)
+      run(type, std::true_type{}, std::true_type{});
+    else
+      run(type, std::true_type{}, std::false_type{});
   };
   if (a.f32)
-    a.top ? run(float{}, std::true_type{}) : run(float{}, std::false_type{});
+    run_type(float{});
   else
-    a.top ? run(__bf16{}, std::true_type{}) : run(__bf16{}, std::false_type{});
+    run_type(__bf16{});
   return hipGetLastError();
 }
 

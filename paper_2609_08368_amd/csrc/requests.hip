@@ -35,15 +35,16 @@ struct Fork {
   int len, kv;                                      // tokens it takes over, tokens it holds without
 };
 __device__ __forceinline__ Fork read_fork(const ForkArgs& a, int b, int* bad) {
-  const int kv = a.kv_lens[(int64_t)b * a.kv_s];
+  const int kv = a.kv_lens[(int64_t)b * a.kv_s], n = a.fork_lens[(int64_t)b * a.fl_s];
   const int p = a.parents[(int64_t)b * a.par_s];
   if (p < 0) return {-1, 0, kv};
+  const int q = min(p, a.B - 1);                    // (read at once with the parent's length)
+  const int theirs = a.kv_lens[(int64_t)q * a.kv_s], grandparent = a.parents[(int64_t)q * a.par_s];
   // from another request that is not forked itself, into one that holds nothing
-  if (p >= a.B || p == b || kv != 0 || a.parents[(int64_t)p * a.par_s] >= 0) {
+  if (p >= a.B || p == b || kv != 0 || grandparent >= 0) {
     *bad |= kErrParent;
     return {-1, 0, kv};
   }
-  const int n = a.fork_lens[(int64_t)b * a.fl_s], theirs = a.kv_lens[(int64_t)p * a.kv_s];
   if (n < 0 || n > theirs || theirs > a.max_pages * a.page_size) {
     *bad |= kErrLen;
     return {-1, 0, kv};
@@ -157,70 +158,164 @@ __global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(CopyArgs a) {
     if (i0 + k * kCopyThreads < n) *reinterpret_cast<u32x4*>(to + off[k]) = x[k];
 }
 
-// Drop: one workgroup marks the pages that requests keep and those they drop, in
-// LDS, and lists the ones dropped and not kept, in the order of their ids.
-constexpr int kDropThreads = 1024;
-constexpr int kDropBits = 7680 * 32;                // pages of a pass (two marks each: 60 KB)
+// The calling waves' requests, first, first + step, ...: a wave calls mark(page, kept)
+// for their pages, and writes the length each keeps (which nobody else reads). Eight
+// loads are under way at once, of one request's entries or of several requests'.
+template <typename Mark>
+__device__ __forceinline__ void for_pages(const DropArgs& a, int first, int step, bool write, int* bad, Mark mark) {
+  constexpr int kAhead = 8;
+  const int lane = threadIdx.x & 63, room = a.max_pages * a.page_size;
+  const int log2_each = a.max_pages <= 64 ? 0 : a.max_pages <= 128 ? 1 : a.max_pages <= 256 ? 2 : 3;
+  const int each = 1 << log2_each, together = kAhead >> log2_each;        // loads of a request, requests
+  for (int b0 = first; b0 < a.B; b0 += step * together) {
+    int page[kAhead], held[kAhead], kept[kAhead];
+    // (entries past a request's are read and not used: one round trip less)
+    if (a.max_pages > 0)
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int b = min(b0 + (i >> log2_each) * step, a.B - 1), j = lane + 64 * (i & (each - 1));
+        page[i] = a.bt[(int64_t)b * a.bt_sb + (int64_t)min(j, a.max_pages - 1) * a.bt_sj];
+      }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int b = b0 + (i >> log2_each) * step, at = min(b, a.B - 1);
+      const int kv = a.kv_lens[(int64_t)at * a.kv_s], k = a.keep_lens[(int64_t)at * a.keep_s];
+      if (kv < 0 || kv > room || k < 0) *bad |= kErrLen;
+      const int len = kv < 0 || b >= a.B ? 0 : min(kv, room), keep = k < 0 ? len : min(k, len);
+      held[i] = (int)(((unsigned)len + a.page_size - 1) >> a.log2_page);
+      kept[i] = (int)(((unsigned)keep + a.page_size - 1) >> a.log2_page);
+    }
+    auto mark_all = [&](int j0) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int j = j0 + 64 * (i & (each - 1));
+        if (j >= held[i]) continue;
+        if ((unsigned)page[i] >= (unsigned)a.num_pages)
+          *bad |= kErrPage;
+        else
+          mark(page[i], j < kept[i]);
+      }
+    };
+    mark_all(lane);
+    for (int j0 = lane + 64 * kAhead; j0 < held[0]; j0 += 64 * kAhead) {  // (then each == kAhead)
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        page[i] = a.bt[(int64_t)b0 * a.bt_sb + (int64_t)min(j0 + 64 * i, held[0] - 1) * a.bt_sj];
+      mark_all(j0);
+    }
+    if (write && lane < together) {                 // (behind the reads: in place)
+      const int b = b0 + lane * step;
+      if (b < a.B) {
+        const int kv = a.kv_lens[(int64_t)b * a.kv_s], k = a.keep_lens[(int64_t)b * a.keep_s];
+        a.kv_out[(int64_t)b * a.kv_out_s] = k < 0 ? kv : min(kv, k);
+      }
+    }
+  }
+}
+
+// Lists the pages of n words (64 bits each, in LDS) of marks, the first of which is
+// page `first`, in the order of their ids up to entry end - 1; returns how many there
+// are. A wave has a word at a time, a lane a bit, so the entries leave it side by side
+// (a thread that had a word and a bit after the other took twice the call's time).
+// base: n ints of LDS. All threads call it.
+constexpr int kDropThreads = 1024, kDropWaves = kDropThreads / 64;
+__device__ __forceinline__ int list_pages(const DropArgs& a, const uint64_t* marks, int n, int* base, int first, int end,
+                                          int* wave_tot) {
+  const int tid = threadIdx.x, lane = tid & 63, each = (n + kDropThreads - 1) / kDropThreads;
+  const int i0 = min(n, tid * each), i1 = min(n, i0 + each);
+  int mine = 0, total;
+  for (int i = i0; i < i1; ++i) mine += __popcll(marks[i]);
+  int at = block_exclusive_scan(mine, &total, wave_tot);
+  for (int i = i0; i < i1; ++i) {
+    base[i] = at;
+    at += __popcll(marks[i]);
+  }
+  __syncthreads();
+  const int start = end - total;
+#pragma unroll 4
+  for (int i = tid >> 6; i < n; i += kDropWaves) {
+    const uint64_t x = marks[i];
+    const int below = __builtin_amdgcn_mbcnt_hi((unsigned)(x >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)x, 0));
+    const int to = start + base[i] + below;
+    if ((x >> lane & 1) && to >= 0) a.free_pages[(int64_t)to * a.free_s] = first + 64 * i + lane;
+  }
+  return total;
+}
+
+__device__ __forceinline__ void finish_drop(const DropArgs& a, int used, int listed, int bad) {
+  if (listed > used) bad |= kErrPool;               // more than the list has lost
+  if (threadIdx.x == 0) *a.used_out = max(0, used - listed);
+  if (bad) atomicOr(a.err, bad);
+}
+
+// The workgroups mark the pages that their requests keep and those they drop, in LDS,
+// and hand the marks to the last one to arrive, which lists the pages dropped and not
+// kept. (Marking in memory took 17 us where this takes 14: an atomic on
+// memory that eight dies share leaves at 3.5 a ns.)
 __global__ __launch_bounds__(kDropThreads) void drop_kernel(DropArgs a) {
-  extern __shared__ unsigned marks[];               // kept, dropped
+  extern __shared__ uint64_t marks[];               // n words of kept pages, n of dropped ones
   __shared__ int wave_tot[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int last;
+  const int tid = threadIdx.x, wave = tid >> 6, n = (a.num_pages + 127) / 128 * 2, groups = gridDim.x;
+  unsigned* bits = reinterpret_cast<unsigned*>(marks);
   int bad = 0;
   const int used = read_used(a.free_used, a.n_free, &bad);
-  const int room = a.max_pages * a.page_size;
-  int found = 0;                                    // pages of all passes
-  // two turns over the pool where it takes several passes: their number first, which says
-  // where the list begins
-  const int passes = max(1, (a.num_pages + kDropBits - 1) / kDropBits);
-  for (int turn = passes > 1 ? 0 : 1, at = 0; turn < 2; ++turn, at = 0)
-    for (int pass = 0; pass < passes; ++pass) {
-      const int first = pass * kDropBits, pages = min(a.num_pages - first, kDropBits);
-      const int words = (pages + 31) / 32;
-      for (int i = tid; i < 2 * words; i += kDropThreads) marks[i] = 0;
-      __syncthreads();
-      for (int b = wave; b < a.B; b += kDropThreads / 64) {       // a wave has a request
-        const int kv = a.kv_lens[(int64_t)b * a.kv_s], k = a.keep_lens[(int64_t)b * a.keep_s];
-        if (kv < 0 || kv > room || k < 0) bad |= kErrLen;
-        const int len = kv < 0 ? 0 : min(kv, room), keep = k < 0 ? len : min(k, len);
-        const int held = (int)(((unsigned)len + a.page_size - 1) >> a.log2_page);
-        const int kept = (int)(((unsigned)keep + a.page_size - 1) >> a.log2_page);
-        for (int j = lane; j < held; j += 64) {
-          const int page = a.bt[(int64_t)b * a.bt_sb + (int64_t)j * a.bt_sj];
-          if ((unsigned)page >= (unsigned)a.num_pages) {
-            bad |= kErrPage;
-            continue;
-          }
-          const int i = page - first;
-          if ((unsigned)i < (unsigned)pages) atomicOr(&marks[(j < kept ? 0 : words) + (i >> 5)], 1u << (i & 31));
-        }
-      }
-      __syncthreads();
-      const int each = (words + kDropThreads - 1) / kDropThreads;
-      const int w0 = min(words, tid * each), w1 = min(words, w0 + each);
-      int mine = 0;
-      for (int i = w0; i < w1; ++i) mine += __popc(marks[words + i] & ~marks[i]);
-      int total;
-      int rank = at + block_exclusive_scan(mine, &total, wave_tot);
-      at += total;
-      if (passes == 1) found = total;
-      if (turn == 0) {
-        found += total;
-      } else {
-        for (int i = w0; i < w1; ++i)
-          for (unsigned m = marks[words + i] & ~marks[i]; m; m &= m - 1, ++rank) {
-            const int to = used - found + rank;
-            if (to >= 0) a.free_pages[(int64_t)to * a.free_s] = first + 32 * i + __ffs(m) - 1;
-          }
-      }
-      __syncthreads();
+  for (int i = tid; i < 2 * n; i += kDropThreads) marks[i] = 0;
+  __syncthreads();
+  for_pages(a, blockIdx.x * kDropWaves + wave, groups * kDropWaves, true, &bad,
+            [&](int page, bool keep) { atomicOr(&bits[(keep ? 0 : 2 * n) + (page >> 5)], 1u << (page & 31)); });
+  __syncthreads();
+  if (groups > 1) {
+    uint64_t* mine = a.marks + (int64_t)blockIdx.x * 2 * n;
+    for (int i = tid; i < 2 * n; i += kDropThreads) hand_over(mine + i, marks[i]);
+    if (!arrive(a.arrived, groups, &last)) {
+      if (bad) atomicOr(a.err, bad);
+      return;
     }
-  for (int b = tid; b < a.B; b += kDropThreads) {
-    const int kv = a.kv_lens[(int64_t)b * a.kv_s], k = a.keep_lens[(int64_t)b * a.keep_s];
-    a.kv_out[(int64_t)b * a.kv_out_s] = k < 0 ? kv : min(kv, k);
   }
-  if (found > used) bad |= kErrPool;                // more than the list has lost
-  if (tid == 0) *a.used_out = max(0, used - found);
-  if (bad) atomicOr(a.err, bad);
+  if (groups > 1) {
+    for (int i = tid; i < 2 * n; i += kDropThreads) {
+      uint64_t x = 0;
+#pragma unroll
+      for (int g = 0; g < kDropGroups; ++g)         // (all under way at once; the last one again where there are fewer)
+        x |= handed_over(a.marks + (int64_t)min(g, groups - 1) * 2 * n + i);
+      marks[i] = x;
+    }
+    __syncthreads();
+  }
+  for (int i = tid; i < n; i += kDropThreads) marks[i] = marks[n + i] & ~marks[i];
+  __syncthreads();
+  const int listed = list_pages(a, marks, n, reinterpret_cast<int*>(marks + n), 0, used, wave_tot);
+  finish_drop(a, used, listed, bad);
+}
+
+// Larger pools: one workgroup, a part of the pool after the other, from the highest ids
+// down (so that their number need not be known before).
+__global__ __launch_bounds__(kDropThreads) void drop_large_kernel(DropArgs a) {
+  extern __shared__ uint64_t marks[];               // kept, dropped
+  __shared__ int wave_tot[16];
+  const int tid = threadIdx.x, wave = tid >> 6;
+  constexpr int n = kDropPart / 64;
+  unsigned* bits = reinterpret_cast<unsigned*>(marks);
+  int bad = 0;
+  const int used = read_used(a.free_used, a.n_free, &bad);
+  int listed = 0;
+  for (int part = (a.num_pages - 1) / kDropPart; part >= 0; --part) {
+    const int first = part * kDropPart;
+    for (int i = tid; i < 2 * n; i += kDropThreads) marks[i] = 0;
+    __syncthreads();
+    // (in place, the lengths are there until the last part has been read)
+    for_pages(a, wave, kDropWaves, part == 0, &bad, [&](int page, bool keep) {
+      const int i = page - first;
+      if ((unsigned)i < (unsigned)kDropPart) atomicOr(&bits[(keep ? 0 : 2 * n) + (i >> 5)], 1u << (i & 31));
+    });
+    __syncthreads();
+    for (int i = tid; i < n; i += kDropThreads) marks[i] = marks[n + i] & ~marks[i];
+    __syncthreads();
+    listed += list_pages(a, marks, n, reinterpret_cast<int*>(marks + n), first, used - listed, wave_tot);
+    __syncthreads();
+  }
+  finish_drop(a, used, listed, bad);
 }
 
 }  // namespace
@@ -252,8 +347,14 @@ hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_drop(const DropArgs& a, hipStream_t stream) {
-  const int words = (std::min(a.num_pages, kDropBits) + 31) / 32;
-  drop_kernel<<<1, kDropThreads, 2 * sizeof(unsigned) * (size_t)words, stream>>>(a);
+  if (a.num_pages <= kDropPart) {
+    const int bytes = (a.num_pages + 127) / 128 * 32;
+    // as many workgroups as there are requests for, and room for their marks
+    const int groups = std::max(1, std::min({kDropGroups, (a.B + 15) / 16, kDropMarkBytes / std::max(bytes, 1)}));
+    drop_kernel<<<groups, kDropThreads, (size_t)bytes, stream>>>(a);
+  } else {
+    drop_large_kernel<<<1, kDropThreads, kDropPart / 4, stream>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -255,13 +255,18 @@ struct Workspace {
   size_t size = 0;
   void* stash = nullptr;
   size_t refused = SIZE_MAX;   // a size that could not be allocated: not tried again for what is merely wanted
-  int* err = nullptr;
+  int* err = nullptr;          // the error word, and behind it counters and marks
   // set once a call on this stream was captured into a graph: the graph keeps
   // the buffer's address, so a later growth retires the buffer (freed by
   // rl_attn_release) instead of freeing it
   bool captured = false;
   std::vector<void*> retired;
 };
+
+// The block of an error word: the word, a counter of workgroups, then counters of rows (0 between calls) and marks of
+// pages.
+constexpr size_t kErrRowCounters = 256, kErrMarks = kErrRowCounters + rl::kLogprobSharedRows * sizeof(int);
+constexpr size_t kErrBlockBytes = kErrMarks + rl::kDropMarkBytes;
 
 std::mutex g_mu;
 std::map<std::pair<int, hipStream_t>, Workspace> g_ws;
@@ -314,9 +319,10 @@ int acquire_ws(hipStream_t st, size_t need, size_t want, bool need_stash, Worksp
   }
   if (need_err) {
     void* p = nullptr;
-    e = hipMalloc(&p, 256);
-    if (e != hipSuccess) return fail(RL_ERR_WORKSPACE, "hipMalloc(256) for the error word failed: %s", hipGetErrorString(e));
-    e = hipMemset(p, 0, 256);
+    e = hipMalloc(&p, kErrBlockBytes);
+    if (e != hipSuccess)
+      return fail(RL_ERR_WORKSPACE, "hipMalloc(%zu) for the error word failed: %s", kErrBlockBytes, hipGetErrorString(e));
+    e = hipMemset(p, 0, kErrBlockBytes);
     if (e != hipSuccess) return hip_fail(e, "hipMemset");
     w.err = static_cast<int*>(p);
   }
@@ -1574,6 +1580,7 @@ int logprobs_impl(const rl_tensor* logits, const rl_tensor* tokens, const rl_ten
   Workspace* w = nullptr;
   RL_TRY(acquire_ws(st, need, need, false, &w));
   a.parts = w->ptr;
+  a.arrived = w->err + kErrRowCounters / sizeof(int);
   a.cands = need ? reinterpret_cast<uint64_t*>(static_cast<char*>(w->ptr) + l.cands) : nullptr;
   a.logprobs = static_cast<float*>(logprobs->data);
   a.lp_s = logprobs->strides[0];
@@ -1818,6 +1825,8 @@ int drop_impl(const rl_tensor* kv_lens, const rl_tensor* keep_lens, const rl_ten
   while ((1 << a.log2_page) < page_size) ++a.log2_page;
   a.max_pages = (int)block_table->shape[1];
   a.err = w->err;
+  a.arrived = w->err + 32;
+  a.marks = reinterpret_cast<uint64_t*>(w->err + kErrMarks / sizeof(int));
   const hipError_t e = rl::launch_drop(a, st);
   if (e != hipSuccess) return hip_fail(e, "drop kernel launch");
   return RL_OK;

@@ -43,40 +43,57 @@ __global__ __launch_bounds__(kGradThreads) void rope_grad_kernel(RopeGradArgs a)
     atomicOr(a.r.err, kErrAxis);
     axis = axis < 0 ? 0 : a.r.n_axes - 1;
   }
-  f32x8 sa = {}, sb = {};
-  for (int u = group * kGradWaves + wave; u < units; u += groups * kGradWaves) {
+  // a unit's rows and position; those of the next are loaded before this one's are used
+  struct Unit {
+    bf16x8 xa, xb, ga, gb;
+    int64_t r;
+    int h, at;
+    bool has;
+  };
+  auto load = [&](int u) {
+    Unit t;
     const int r32 = u / parts;
-    const int64_t r = r32;
-    const int h = (u - r32 * parts) * 8 + (lane >> 3);
-    const bool has = h < heads;
-    const int at = a.r.pos[(int64_t)min(lane, a.r.n_axes - 1) * a.r.pos_sa + r * a.r.pos_st];
-    bf16x8 xa = zero_bf16x8(), xb = xa, ga = xa, gb = xa;
-    if (has) {
-      const __bf16* px = x + r * x_st + h * x_sh;
-      const __bf16* pg = dy + r * dy_st + h * dy_sh;
-      xa = load_nt<bf16x8>(px + c.lo);
-      xb = load_nt<bf16x8>(px + c.hi);
-      ga = load_nt<bf16x8>(pg + c.lo);
-      gb = load_nt<bf16x8>(pg + c.hi);
+    t.r = r32;
+    t.h = (u - r32 * parts) * 8 + (lane >> 3);
+    t.has = t.h < heads;
+    t.xa = t.xb = t.ga = t.gb = zero_bf16x8();
+    t.at = a.r.pos[(int64_t)min(lane, a.r.n_axes - 1) * a.r.pos_sa + t.r * a.r.pos_st];
+    if (t.has) {
+      const __bf16* px = x + t.r * x_st + t.h * x_sh;
+      const __bf16* pg = dy + t.r * dy_st + t.h * dy_sh;
+      t.xa = load_nt<bf16x8>(px + c.lo);
+      t.xb = load_nt<bf16x8>(px + c.hi);
+      t.ga = load_nt<bf16x8>(pg + c.lo);
+      t.gb = load_nt<bf16x8>(pg + c.hi);
     }
-    const int p = __shfl(at, axis);
+    return t;
+  };
+  f32x8 sa = {}, sb = {};
+  const int step = groups * kGradWaves;
+  int u = group * kGradWaves + wave;
+  Unit next;
+  if (u < units) next = load(u);
+  for (; u < units; u += step) {
+    const Unit t = next;
+    if (u + step < units) next = load(u + step);
+    const int p = __shfl(t.at, axis);
     __builtin_amdgcn_wave_barrier();                // (the last unit's angles have been read)
     cs[wave][lane] = cos_sin_turns((double)p * turns);
     __builtin_amdgcn_wave_barrier();
-    f32x8 na = widen(xa), nb = widen(xb), ya = widen(ga), yb = widen(gb);
+    f32x8 na = widen(t.xa), nb = widen(t.xb), ya = widen(t.ga), yb = widen(t.gb);
     if (c.turned) {
-      float2 t[8];
+      float2 cosines[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] = cs[wave][8 * d + e];
-      turn(ya, yb, t, a.r.interleaved);
+      for (int e = 0; e < 8; ++e) cosines[e] = cs[wave][8 * d + e];
+      turn(ya, yb, cosines, a.r.interleaved);
     }
     const float rms = inv_rms(na, nb, a.r.eps);
     na *= rms;
     nb *= rms;
     const f32x8 ua = ya * wa, ub = yb * wb;
     const float mean = row_sum8(dot16(ua, na, ub, nb)) * (1.f / kHeadDim);
-    if (has) {
-      __bf16* pd = dx + r * dx_st + h * dx_sh;
+    if (t.has) {
+      __bf16* pd = dx + t.r * dx_st + t.h * dx_sh;
       store_chunk<true>(pd + c.lo, narrow((ua - na * mean) * rms));
       store_chunk<true>(pd + c.hi, narrow((ub - nb * mean) * rms));
       sa += ya * na;
@@ -104,26 +121,28 @@ __global__ __launch_bounds__(kGradThreads) void rope_grad_kernel(RopeGradArgs a)
   }
 }
 
-// Workgroup 0: the weights of q; 1: those of k.
-constexpr int kSumThreads = 1024, kSumRows = kSumThreads / kHeadDim;
+// Workgroup: sixteen columns of the sums of q (y = 0) or k; a thread's loads are in
+// flight together, as few workgroups have much to read.
+constexpr int kSumThreads = 1024, kSumCols = 16, kSumRows = kSumThreads / kSumCols;
 __global__ __launch_bounds__(kSumThreads) void rope_grad_sum_kernel(RopeGradArgs a) {
-  __shared__ float sums[kSumRows][kHeadDim];
-  const int i = threadIdx.x % kHeadDim, j = threadIdx.x / kHeadDim;
-  const bool is_k = blockIdx.x != 0;
+  __shared__ float sums[kSumRows][kSumCols + 1];
+  const int i = threadIdx.x % kSumCols, j = threadIdx.x / kSumCols, col = blockIdx.x * kSumCols + i;
+  const bool is_k = blockIdx.y != 0;
   const int first = is_k ? a.q_groups : 0, end = is_k ? a.q_groups + a.k_groups : a.q_groups;
   float s = 0.f;
-#pragma unroll 8
-  for (int g = first + j; g < end; g += kSumRows) s += a.parts[(int64_t)g * kHeadDim + i];
+#pragma unroll 16
+  for (int g = first + j; g < end; g += kSumRows) s += a.parts[(int64_t)g * kHeadDim + col];
   sums[j][i] = s;
   __syncthreads();
+  for (int n = kSumRows / 2; n > 0; n >>= 1) {
+    if (j < n) sums[j][i] += sums[j + n][i];
+    __syncthreads();
+  }
   if (j != 0) return;
-  s = 0.f;
-#pragma unroll
-  for (int k = 0; k < kSumRows; ++k) s += sums[k][i];
   if (is_k)
-    a.dk_weight[i * a.dkw_s] = s;
+    a.dk_weight[col * a.dkw_s] = sums[0][i];
   else
-    a.dq_weight[i * a.dqw_s] = s;
+    a.dq_weight[col * a.dqw_s] = sums[0][i];
 }
 
 }  // namespace
@@ -132,7 +151,7 @@ hipError_t launch_rope_grad(const RopeGradArgs& a, hipStream_t stream, KernelTim
   if (timer) (void)hipEventRecord(timer->start, stream);
   if (a.q_groups + a.k_groups > 0) rope_grad_kernel<<<a.q_groups + a.k_groups, kGradThreads, 0, stream>>>(a);
   if (timer) (void)hipEventRecord(timer->stop, stream);
-  rope_grad_sum_kernel<<<a.dk_weight ? 2 : 1, kSumThreads, 0, stream>>>(a);
+  rope_grad_sum_kernel<<<dim3(kHeadDim / kSumCols, a.dk_weight ? 2 : 1), kSumThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -241,7 +241,7 @@ def test_drop_equals_the_definition(case, in_place):
 
 @pytest.mark.parametrize("spread", [300, 3000])
 def test_drop_in_large_pools(spread):
-    """Ids all over a pool of 334 thousand and of 3.3 million pages."""
+    """Ids all over a pool of 334 thousand pages and of 3.3 million pages."""
     for in_place in (False, True):
         c = drop_case(5, 60, 600, 16, spread=spread)
         want = check_drop(c, in_place)
