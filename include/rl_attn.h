@@ -393,7 +393,7 @@ size_t rl_attn_norm_rope_backward_workspace_size(void);
  *   logits     [T, V] bf16 or f32, V <= 2^21, last stride 1, any row stride (views
  *              of a wider buffer, rows that start at any element)
  *   tokens     [T] int32 or int64. A row with a negative token is left out: its
- *              logits are not read, its outputs are 0, its alternatives -1 and
+ *              logits do not matter, its outputs are 0, its alternatives -1 and
  *              -inf. A token of V or more is reported and its row left out.
  *   row_scale  [T] f32, nullable (1): e.g. one over a temperature, any stride from
  *              0 on; must be positive and finite, else the row is reported and left out

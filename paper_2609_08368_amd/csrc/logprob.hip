@@ -30,11 +30,18 @@ namespace {
 constexpr int kLpThreads = 256, kLpWaves = kLpThreads / 64;
 constexpr int kSegment = kLogprobSegment;
 constexpr int kCand = 512;                          // candidates that are ranked at once
+constexpr int kHeldCand = 64;                       // of a wave, from its registers
+constexpr int kCellRounds = 16;                     // rounds of segments whose largest logits are kept, at most
 constexpr uint32_t kKeyNegInf = 0x007fffffu;        // key_of(-inf)
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 // (rows may start at any element: a vocabulary need not be a multiple of 16 bytes)
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+// 128 registers: left alone the compiler takes 168 and three waves a SIMD fit (512 rows
+// of 131072 bf16 logits with 20 alternatives 43 us, 49 so; 4096 of 32000 68 and 75); 80
+// or 64 leave it spilling (72 and 94).
+constexpr int kLpWavesPerSimd = 4;
 
 // Logits of type X in sixteen bytes, and those as fp32.
 template <typename X>
@@ -125,9 +132,9 @@ __device__ __forceinline__ float above_base(float m, float c) {
 template <typename X>
 constexpr int kLoads = kSegment / 64 / kPer<X>;
 
-// A wave's segment of n logits at x, left in w; *lane_max is the largest of this lane's.
+// A wave's segment of n logits at x, to registers.
 template <typename X>
-__device__ __forceinline__ Part segment_part(const X* x, int n, float c, u32x4 (&w)[kLoads<X>], float* lane_max) {
+__device__ __forceinline__ void load_segment(const X* x, int n, u32x4 (&w)[kLoads<X>]) {
   const int at = (threadIdx.x & 63) * kPer<X>;
   if (n == kSegment) {
 #pragma unroll
@@ -137,6 +144,11 @@ __device__ __forceinline__ Part segment_part(const X* x, int n, float c, u32x4 (
 #pragma unroll
     for (int i = 0; i < kLoads<X>; ++i) w[i] = load_logits(x, at + i * 64 * kPer<X>, n);
   }
+}
+
+// The sums of a wave's segment; *lane_max is the largest of this lane's logits.
+template <typename X>
+__device__ __forceinline__ Part segment_part(const u32x4 (&w)[kLoads<X>], float c, float* lane_max) {
   float top = kNegInf;
 #pragma unroll
   for (int i = 0; i < kLoads<X>; ++i) {
@@ -245,27 +257,34 @@ __device__ __forceinline__ void write_masked(const LogprobArgs& a, int64_t r) {
 
 struct TopLds {
   __attribute__((aligned(16))) uint32_t keys[kLpThreads];
-  uint64_t cand[kCand];
+  __attribute__((aligned(16))) uint64_t cand[kCand];
   uint64_t best[kLogprobTop];
   uint32_t tau;
-  int winners[kLpThreads];
+  union {
+    int winners[kCand];                             // rounds << 8 | threads whose logits are read again
+    uint64_t mine[kLpWaves][kHeldCand];             // of each wave
+  };
   int n_winners, n_cand;
 };
 
 // The `top` largest of t.cand[0 .. n) to t.best, in order; 0 behind the last. (Each
 // counts the larger ones; reads of a fixed number at a time overlap.)
 __device__ __forceinline__ void rank_candidates(TopLds& t, int n, int top) {
+  typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
   const int tid = threadIdx.x;
-  const int padded = (n + 7) & ~7;                  // (kCand is a multiple of 8)
+  const int padded = (n + 15) & ~15;                // (kCand is a multiple of 16)
   if (tid < top) t.best[tid] = 0;
   if (tid < padded - n) t.cand[n + tid] = 0;
   __syncthreads();
   for (int i = tid; i < n; i += kLpThreads) {
     const uint64_t mine = t.cand[i];
     int rank = 0;
-    for (int j = 0; j < padded; j += 8) {
+    for (int j = 0; j < padded; j += 16) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) rank += t.cand[j + k] > mine;
+      for (int k = 0; k < 16; k += 2) {
+        const u64x2 two = *reinterpret_cast<const u64x2*>(&t.cand[j + k]);
+        rank += (two.x > mine) + (two.y > mine);
+      }
     }
     if (mine != 0 && rank < top) t.best[rank] = mine;
   }
@@ -273,23 +292,27 @@ __device__ __forceinline__ void rank_candidates(TopLds& t, int n, int top) {
 }
 
 // A bound that at least `top` of the workgroup's threads' largest logits reach, and
-// hardly more: bit by bit from the top, until the count is near enough.
+// hardly more: two bits after two from the top, until the count is near enough.
 __device__ __forceinline__ void find_bound(TopLds& t, float lane_max, int top) {
   constexpr int kSlack = 8;                         // (a few more to look at cost less than more bits)
   const int tid = threadIdx.x;
   t.keys[tid] = key_of(lane_max);
   __syncthreads();
   if (tid < 64) {
-    const u32x4 k = *reinterpret_cast<const u32x4*>(&t.keys[4 * tid]);
+    const u32x4 w = *reinterpret_cast<const u32x4*>(&t.keys[4 * tid]);
     uint32_t lo = 0;
-    for (uint32_t bit = 0x80000000u; bit != 0; bit >>= 1) {
-      const uint32_t next = lo | bit;
-      int n = 0;
+    for (int shift = 30; shift >= 0; shift -= 2) {
+      int n[4];                                     // threads that reach lo + k steps
 #pragma unroll
-      for (int i = 0; i < 4; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(k[i] >= next));
-      if (n < top) continue;
-      lo = next;
-      if (n <= top + kSlack) break;
+      for (int k = 1; k < 4; ++k) {
+        const uint32_t next = lo | (uint32_t)k << shift;
+        n[k] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[k] += __popcll(__builtin_amdgcn_ballot_w64(w[i] >= next));
+      }
+      const int k = n[3] >= top ? 3 : n[2] >= top ? 2 : n[1] >= top ? 1 : 0;
+      lo |= (uint32_t)k << shift;
+      if (k > 0 && (k == 3 ? n[3] : k == 2 ? n[2] : n[1]) <= top + kSlack) break;
     }
     if (tid == 0) {
       t.tau = max(lo, kKeyNegInf + 1);              // excluded tokens are no alternatives
@@ -320,26 +343,72 @@ __device__ __forceinline__ void add_candidates(TopLds& t, u32x4 w, int e, uint32
 // thread's largest logit of those. kHeld: each wave has one, which is in w.
 template <typename X, bool kHeld>
 __device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int seg0, int seg1, float lane_max,
-                                         const u32x4 (&w)[kLoads<X>], int top) {
+                                         const u32x4 (&w)[kLoads<X>], const u16* cells, int top) {
   const int tid = threadIdx.x;
   find_bound(t, lane_max, top);
   const uint32_t tau = t.tau;
   const bool wins = key_of(lane_max) >= tau;
+  static_assert(kCand >= kLpWaves * kHeldCand, "every wave's list fits");
   if constexpr (kHeld) {
-    if (wins) {
-      const int e = (seg0 + (tid >> 6)) * kSegment + (tid & 63) * kPer<X>;
+    // a wave lists its own side by side, and then takes room for them at once
+    const int lane = tid & 63, wave = tid >> 6;
+    int n = 0;
+    if (__builtin_amdgcn_ballot_w64(wins) != 0) {
+      const float bound = float_of(tau);
+      const int e = (seg0 + wave) * kSegment + lane * kPer<X>;
 #pragma unroll
-      for (int i = 0; i < kLoads<X>; ++i) add_candidates<X>(t, w[i], e + i * 64 * kPer<X>, tau);
+      for (int i = 0; i < kLoads<X>; ++i) {
+        float f[kPer<X>];
+        unpack<X>(w[i], f);
+#pragma unroll
+        for (int j = 0; j < kPer<X>; ++j) {
+          if (__builtin_amdgcn_ballot_w64(wins && f[j] >= bound) == 0) continue;
+          const uint32_t k = key_of(f[j]);          // (NaN may pass the bound, and its key does not)
+          const bool in = wins && k >= tau;
+          const uint64_t m = __builtin_amdgcn_ballot_w64(in);
+          const int at = n + __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
+          if (in && at < kHeldCand) t.mine[wave][at] = rank_of(k, e + i * 64 * kPer<X> + j);
+          n += __popcll(m);
+        }
+      }
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&t.n_cand, n > kHeldCand ? kCand + 1 : n);
+      at = __builtin_amdgcn_readfirstlane(at);
+      __builtin_amdgcn_wave_barrier();
+      if (lane < n && at + lane < kCand) t.cand[at + lane] = t.mine[wave][lane];
     }
   } else {
-    if (wins) t.winners[atomicAdd(&t.n_winners, 1)] = tid;
+    // a thread's logits of those rounds whose largest reaches the bound, if that is
+    // kept (cells: its upper half), else of all
+    const int rounds = (seg1 - seg0 + kLpWaves - 1) / kLpWaves;
+    if (wins)
+      for (int i = 0; i < (cells ? rounds : 1); ++i) {
+        if (seg0 + (tid >> 6) + i * kLpWaves >= seg1) break;
+        if (cells && cells[i * kLpThreads + tid] < (tau >> 16)) continue;
+        const int at = atomicAdd(&t.n_winners, 1);
+        if (at < kCand) t.winners[at] = i << 8 | tid;
+      }
     __syncthreads();
-    const int rounds = (seg1 - seg0 + kLpWaves - 1) / kLpWaves, per = rounds * kLoads<X>, n = t.n_winners * per;
-    for (int p = tid; p < n; p += kLpThreads) {
-      const int who = t.winners[p / per], i = p % per;
-      const int seg = seg0 + (who >> 6) + (i / kLoads<X>) * kLpWaves;
-      const int e = seg * kSegment + ((i % kLoads<X>) * 64 + (who & 63)) * kPer<X>;
-      if (seg < seg1 && e < vocab) add_candidates<X>(t, load_logits(x, e, vocab), e, tau);
+    const int per = (cells ? 1 : rounds) * kLoads<X>, n = min(t.n_winners, kCand) * per;
+    if (t.n_winners > kCand && tid == 0) t.n_cand = kCand + 1;
+    constexpr int kAgain = 4;                       // loads that are under way at once
+    for (int p0 = tid; p0 < n; p0 += kAgain * kLpThreads) {
+      u32x4 again[kAgain];
+      int e[kAgain];
+#pragma unroll
+      for (int k = 0; k < kAgain; ++k) {
+        const int p = p0 + k * kLpThreads;
+        e[k] = vocab;
+        if (p < n) {
+          const int entry = t.winners[p / per], i = p % per, who = entry & (kLpThreads - 1);
+          const int seg = seg0 + (who >> 6) + ((entry >> 8) + i / kLoads<X>) * kLpWaves;
+          if (seg < seg1) e[k] = seg * kSegment + ((i % kLoads<X>) * 64 + (who & 63)) * kPer<X>;
+        }
+        again[k] = load_logits(x, e[k], vocab);
+      }
+#pragma unroll
+      for (int k = 0; k < kAgain; ++k)
+        if (e[k] < vocab) add_candidates<X>(t, again[k], e[k], tau);
     }
   }
   __syncthreads();
@@ -387,13 +456,22 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, int64_t r, const
 // segments' sums and their likeliest tokens in memory, and the last of them to
 // arrive answers. kHeld: a wave has one segment at most.
 template <typename X, bool kTop, bool kHeld>
-__global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobArgs a) {
-  extern __shared__ Part parts[];                   // a workgroup for each row: [segs]
+__global__ __launch_bounds__(kLpThreads, kLpWavesPerSimd) void logprob_kernel(LogprobArgs a) {
+  extern __shared__ Part parts[];                   // a workgroup for each row: [segs]; behind them, cells
   __shared__ TopLds top;
   __shared__ int last;
   const int row32 = blockIdx.x / a.chunks, chunk = blockIdx.x - row32 * a.chunks;
   const int64_t r = row32;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const X* x = static_cast<const X*>(a.x) + r * a.x_s;
+  const int seg0 = chunk * a.segs_chunk, seg1 = min(a.segs, seg0 + a.segs_chunk);
+  Part* shared = a.chunks > 1 ? static_cast<Part*>(a.parts) + r * a.segs : nullptr;
+  u32x4 w[kLoads<X>];
+  auto load = [&](int s) { load_segment(x + s * kSegment, min(kSegment, a.vocab - s * kSegment), w); };
+  // (calls of few rows do not wait for the token before they load; of many, rows that
+  // are left out are not loaded)
+  int s = seg0 + wave;
+  if (shared && s < seg1) load(s);
   int bad = 0;
   const RowInput in = read_row(a, r, &bad);
   if (in.token < 0) {
@@ -402,16 +480,20 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobArgs a) {
     write_masked(a, r);
     return;
   }
-  const X* x = static_cast<const X*>(a.x) + r * a.x_s;
   const float c = in.scale * kLog2e, x_token = (float)x[in.token];
-  const int seg0 = chunk * a.segs_chunk, seg1 = min(a.segs, seg0 + a.segs_chunk);
-  Part* shared = a.chunks > 1 ? static_cast<Part*>(a.parts) + r * a.segs : nullptr;
+  if (!shared && s < seg1) load(s);
   float most = kNegInf;
-  u32x4 w[kLoads<X>];
-  for (int s = seg0 + wave; s < seg1; s += kLpWaves) {
+  u16* cells = nullptr;                             // upper halves of the threads' largest of each round
+  if (kTop && !kHeld && a.segs_chunk <= kLpWaves * kCellRounds)
+    cells = reinterpret_cast<u16*>(parts + (shared ? 0 : a.segs)) + tid;
+  while (s < seg1) {
     float lane_max;
-    const Part p = segment_part(x + s * kSegment, min(kSegment, a.vocab - s * kSegment), c, w, &lane_max);
+    const Part p = segment_part<X>(w, c, &lane_max);
     most = fmaxf(most, lane_max);
+    if (kTop && !kHeld && cells) {
+      *cells = (u16)(key_of(lane_max) >> 16);
+      cells += kLpThreads;
+    }
     if ((tid & 63) == 0) {
       if (shared) {
         hand_over(&shared[s].m, p.m);
@@ -422,8 +504,11 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobArgs a) {
       }
     }
     if (kHeld) break;
+    s += kLpWaves;
+    if (s < seg1) load(s);
   }
-  if constexpr (kTop) find_top<X, kHeld>(top, x, a.vocab, seg0, seg1, most, w, a.top);
+  if (kTop && !kHeld && cells) cells = reinterpret_cast<u16*>(parts + (shared ? 0 : a.segs));
+  if constexpr (kTop) find_top<X, kHeld>(top, x, a.vocab, seg0, seg1, most, w, cells, a.top);
   Part sums;
   if (shared) {
     uint64_t* cands = a.cands + r * a.chunks * a.top;
@@ -523,7 +608,9 @@ hipError_t launch_logprob(const LogprobArgs& args, hipStream_t stream) {
   a.segs = (a.vocab + kSegment - 1) / kSegment;
   a.segs_chunk = ((a.segs + a.chunks - 1) / a.chunks + kLpWaves - 1) / kLpWaves * kLpWaves;
   const unsigned grid = (unsigned)((int64_t)a.rows * a.chunks);
-  const size_t lds = a.chunks == 1 ? sizeof(Part) * (size_t)a.segs : 0;
+  const size_t lds_parts = a.chunks == 1 ? sizeof(Part) * (size_t)a.segs : 0;
+  const int rounds = a.segs_chunk / kLpWaves;
+  const size_t lds = lds_parts + (a.top && rounds > 1 && rounds <= kCellRounds ? rounds * kLpThreads * sizeof(u16) : 0);
   auto run = [&](auto type, auto top, auto held) {
     logprob_kernel<decltype(type), decltype(top)::value, decltype(held)::value>
         <<<grid, kLpThreads, lds, stream>>>(a);
