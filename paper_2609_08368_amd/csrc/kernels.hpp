@@ -311,7 +311,7 @@ struct RopeGradArgs {
   float* parts;           // [q_groups + k_groups, 128] workgroups' sums of the weights' gradients
   int q_groups, k_groups; // workgroups of q and of k
 };
-constexpr int kRopeGradGroupsPerCu = 4;             // at most
+constexpr int kRopeGradGroupsPerCu = 8;             // at most
 
 // Log probabilities of tokens, and the gradient of their logits.
 constexpr int kLogprobSegment = 4096;               // logits a wave sums at once
