@@ -141,7 +141,10 @@ __global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(CopyArgs a) {
   const int64_t sp = blockIdx.z ? a.vp_sp : a.kp_sp, ss = blockIdx.z ? a.vp_ss : a.kp_ss;
   const int64_t sh = blockIdx.z ? a.vp_sh : a.kp_sh;
   const int per_head = a.row_bytes / 16, per_row = a.Hkv * per_head, n = rows * per_row;
+  // (the rows of a page mostly lie side by side)
+  const bool dense = ss == (int64_t)a.Hkv * a.row_bytes && (sh == a.row_bytes || a.Hkv == 1);
   const int i0 = blockIdx.y * kCopyThreads * kCopyLoads + threadIdx.x;
+  if (i0 >= n) return;
   const char* from = base + src * sp;
   char* to = base + dst * sp;
   u32x4 x[kCopyLoads];
@@ -149,8 +152,11 @@ __global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(CopyArgs a) {
 #pragma unroll
   for (int k = 0; k < kCopyLoads; ++k) {
     const int i = min(i0 + k * kCopyThreads, n - 1);
-    const int t = i / per_row, rem = i - t * per_row, h = rem / per_head;
-    off[k] = t * ss + h * sh + (rem - h * per_head) * 16;
+    off[k] = (int64_t)i * 16;
+    if (!dense) {
+      const int t = i / per_row, rem = i - t * per_row, h = rem / per_head;
+      off[k] = t * ss + h * sh + (rem - h * per_head) * 16;
+    }
     x[k] = *reinterpret_cast<const u32x4*>(from + off[k]);
   }
 #pragma unroll

@@ -310,3 +310,43 @@ def test_gradient_is_the_difference_of_the_kernel():
         diff = ((a.logprobs - b.logprobs) + (a.entropy - b.entropy)).double() / (2 * step) * floats(g).double()
         bound = np.abs(g) * (2 * (300 + 420 * 6) * E / (2 * step) + 2.0 ** -12 * 8 / 6)
         assert np.all(np.abs(H.f64(d[:, j]) - H.f64(diff)) <= bound)
+
+
+def test_outputs_that_are_not_asked_for():
+    """The C call without entropy, lse or alternatives, and a gradient of the entropy alone."""
+    import ctypes
+
+    x, tokens, _ = make(11, 5, 20011, "bf16")
+    t, want = tokens_of(tokens), ra.token_logprobs(x, tokens_of(tokens), top=2)
+    lp = torch.empty(5, device=DEV)
+    views = [None if v is None else ctypes.byref(ra.view(v)) for v in (x, t, None, lp, None, None, None, None)]
+    assert ra.lib().rl_attn_token_logprobs(*views, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(lp, want.logprobs)
+
+
+def test_the_same_call_gives_the_same_bits():
+    """Rows that many workgroups share: whichever arrives last."""
+    x, tokens, _ = make(12, 7, 250007, "bf16")
+    t = tokens_of(tokens)
+    first = ra.token_logprobs(x, t, top=32)
+    for _ in range(200):
+        assert all(torch.equal(a, b) for a, b in zip(ra.token_logprobs(x, t, top=32), first))
+
+
+def test_logits_past_four_gigabytes():
+    """Offsets beyond 32 bits in elements: the last rows give the bits that they give alone, forward and backward."""
+    rows, vocab = 17001, 131073                          # 2.2e9 logits
+    x = torch.zeros((rows, vocab), dtype=torch.bfloat16, device=DEV)
+    some, tokens, _ = make(13, 3, vocab, "bf16")
+    x[-3:] = some
+    t = torch.full((rows,), 5, dtype=torch.int64, device=DEV)
+    t[-3:] = tokens_of(tokens)
+    got, alone = ra.token_logprobs(x, t), ra.token_logprobs(some, t[-3:])
+    for name in ("logprobs", "entropy", "lse"):
+        assert torch.equal(getattr(got, name)[-3:], getattr(alone, name))
+    assert torch.all((got.lse[:-3] - np.log(vocab)).abs() < 1e-5)
+    g = torch.ones(1, device=DEV).expand(rows)
+    d = ra.token_logprobs_backward(some, t[-3:], alone.lse, g[:3])
+    ra.token_logprobs_backward(x, t, got.lse, g, d_logits=x)
+    assert torch.equal(x[-3:], d) and float(x[0, 5]) == pytest.approx(1.0, abs=2 ** -8)
+    assert torch.all(x[rows - 4, 6:] == x[0, 6])        # (the last row of zeros)
