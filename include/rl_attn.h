@@ -47,7 +47,8 @@
  * out-of-range values are counted in a device error word that
  * rl_attn_check_device_errors() reports (as are invalid FP8 dequantisation scales).
  *
- * Memory: the library owns one workspace per (device, stream), grown with
+ * Memory: the library owns one workspace per (device, stream) (and 0.3 MB beside it
+ * for its error word, counters and marks), grown with
  * hipMalloc on demand (or ahead of time with rl_attn_reserve_workspace) and
  * never grown while the stream is being captured (RL_ERR_WORKSPACE instead).
  * A graph captured on a stream uses that stream's workspace when replayed:
@@ -527,7 +528,8 @@ const char* rl_attn_last_error(void);
 /* Synchronises `stream`, then returns RL_ERR_DEVICE if any call on this
  * (device, stream) since the last check met an out-of-range page id, length
  * or indptr on the device (those values were clamped), an invalid FP8 scale,
- * or work beyond its workspace's capacity, RL_OK otherwise, and clears the
+ * a token, scale of a row or fork that its call refuses, or work beyond its
+ * workspace's capacity, RL_OK otherwise, and clears the
  * error word. Errors of rl_attn_decode_noalloc calls on this device are
  * included, whatever their stream. Allocates nothing. */
 int rl_attn_check_device_errors(void* stream);

@@ -12,12 +12,19 @@
 //   lse = s M + ln 2 log2 S,  entropy = ln 2 (log2 S - Y / S)
 // (all terms of one size, none cancelled: Y is taken around the maximum).
 //
-// Alternatives: the K-th largest of a workgroup's threads' maxima is a lower
-// bound of the K-th largest logit, so only the threads whose maximum reaches it
-// hold any of the K likeliest; their logits, about K / 256 of all, are read
-// again, and the few that reach the bound are ranked.
+// Alternatives: a bound that K of a workgroup's threads' largest logits reach bounds
+// the K-th largest logit from below, so only those threads hold any of the K
+// likeliest. Their logits are looked at again (in registers, or read again, and then
+// only those of the segments whose largest reaches the bound), and the few that reach
+// the bound are ranked.
 //
-// A call is one pass over the logits, HBM-bound.
+// A row of a large call is one workgroup's: one pass over the logits, HBM-bound at 6.3
+// TB/s (4096 rows of 131072 bf16 logits, a third left out, 118 us; a large copy runs
+// at 4.9, a read at 7.2). Rows that would not fill the device are shared by up to 16
+// workgroups, the last of which to arrive answers (two launches took 3-4 us more): 128
+// rows of 131072 take 12.6 us, with 20 alternatives 17.8 (38 with a first form that
+// counted larger maxima thread by thread), one row of 32000 6.1 and 10.6, a chain of
+// dependent steps of about 1 us. The gradient is a copy with an exponential: 5.7 TB/s.
 #include <algorithm>
 
 #include "attn_common.hpp"
@@ -340,12 +347,15 @@ __device__ __forceinline__ void add_candidates(TopLds& t, u32x4 w, int e, uint32
 
 // The workgroup's likeliest tokens to t.best: of segments seg0 .. seg1-1 of row x,
 // where wave w has seg0 + w, seg0 + w + kLpWaves, ... and lane_max is this
-// thread's largest logit of those. kHeld: each wave has one, which is in w.
+// thread's largest logit of those. kHeld: each wave has one, which is in w. odd: the
+// wave met a NaN or +inf (a maximum with a signaling NaN may lose what it held, so the
+// bounds do not count then).
 template <typename X, bool kHeld>
-__device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int seg0, int seg1, float lane_max,
+__device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int seg0, int seg1, float lane_max, bool odd,
                                          const u32x4 (&w)[kLoads<X>], const u16* cells, int top) {
   const int tid = threadIdx.x;
   find_bound(t, lane_max, top);
+  if (odd && (tid & 63) == 0) atomicAdd(&t.n_cand, kCand + 1);
   const uint32_t tau = t.tau;
   const bool wins = key_of(lane_max) >= tau;
   static_assert(kCand >= kLpWaves * kHeldCand, "every wave's list fits");
@@ -390,7 +400,7 @@ __device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int s
       }
     __syncthreads();
     const int per = (cells ? 1 : rounds) * kLoads<X>, n = min(t.n_winners, kCand) * per;
-    if (t.n_winners > kCand && tid == 0) t.n_cand = kCand + 1;
+    if (t.n_winners > kCand && tid == 0) atomicAdd(&t.n_cand, kCand + 1);
     constexpr int kAgain = 4;                       // loads that are under way at once
     for (int p0 = tid; p0 < n; p0 += kAgain * kLpThreads) {
       u32x4 again[kAgain];
@@ -417,8 +427,8 @@ __device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int s
     rank_candidates(t, found, top);
     return;
   }
-  // so many equal logits that the list does not hold them: one after the other,
-  // each the largest below the last
+  // odd values, or so many equal logits that the list does not hold them: one after the
+  // other, each the largest below the last
   const int lo = seg0 * kSegment, hi = min(vocab, seg1 * kSegment);
   uint64_t below = ~0ull;
   for (found = 0; found < top; ++found) {
@@ -483,6 +493,7 @@ __global__ __launch_bounds__(kLpThreads, kLpWavesPerSimd) void logprob_kernel(Lo
   const float c = in.scale * kLog2e, x_token = (float)x[in.token];
   if (!shared && s < seg1) load(s);
   float most = kNegInf;
+  bool odd = false;
   u16* cells = nullptr;                             // upper halves of the threads' largest of each round
   if (kTop && !kHeld && a.segs_chunk <= kLpWaves * kCellRounds)
     cells = reinterpret_cast<u16*>(parts + (shared ? 0 : a.segs)) + tid;
@@ -490,6 +501,7 @@ __global__ __launch_bounds__(kLpThreads, kLpWavesPerSimd) void logprob_kernel(Lo
     float lane_max;
     const Part p = segment_part<X>(w, c, &lane_max);
     most = fmaxf(most, lane_max);
+    odd |= (__float_as_uint(p.s) & 0x7fffffffu) > 0x7f800000u;
     if (kTop && !kHeld && cells) {
       *cells = (u16)(key_of(lane_max) >> 16);
       cells += kLpThreads;
@@ -508,7 +520,7 @@ __global__ __launch_bounds__(kLpThreads, kLpWavesPerSimd) void logprob_kernel(Lo
     if (s < seg1) load(s);
   }
   if (kTop && !kHeld && cells) cells = reinterpret_cast<u16*>(parts + (shared ? 0 : a.segs));
-  if constexpr (kTop) find_top<X, kHeld>(top, x, a.vocab, seg0, seg1, most, w, cells, a.top);
+  if constexpr (kTop) find_top<X, kHeld>(top, x, a.vocab, seg0, seg1, most, odd, w, cells, a.top);
   Part sums;
   if (shared) {
     uint64_t* cands = a.cands + r * a.chunks * a.top;

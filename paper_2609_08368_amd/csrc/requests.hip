@@ -10,7 +10,10 @@
 // holds it within the request's tokens, so the tables themselves say which pages
 // are shared, and there are no counts to keep in step with them.
 //
-// The bytes are few; both are chains of dependent loads on top of a launch.
+// The bytes are few; both are chains of dependent loads on top of a launch: 128 forks
+// take 6.2 us, drops of 128 requests with 44K table entries 14, of 3000 with 86K 20.5.
+// The copies are HBM-bound behind their ramp: 128 times 32 rows of 8 heads, K and V, 6.0
+// us, 5.6 TB/s.
 #include <algorithm>
 
 #include "attn_common.hpp"

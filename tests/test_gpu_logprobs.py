@@ -350,3 +350,36 @@ def test_logits_past_four_gigabytes():
     ra.token_logprobs_backward(x, t, got.lse, g, d_logits=x)
     assert torch.equal(x[-3:], d) and float(x[0, 5]) == pytest.approx(1.0, abs=2 ** -8)
     assert torch.all(x[rows - 4, 6:] == x[0, 6])        # (the last row of zeros)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("shape", [(3, 200), (3, 70001), (2050, 9001)], ids=str)
+def test_signaling_nan_hides_no_alternative(shape, kind):
+    """Every NaN pattern, in front of, behind and among a row's largest logits."""
+    rows, vocab = shape
+    x, tokens, _ = make(14, rows, vocab, kind)
+    x[0, 64:72] = torch.arange(30, 38, device=DEV).to(x.dtype)
+    x[1, :8] = 40.0
+    bits = x.view(torch.int16 if kind == "bf16" else torch.int32)
+    patterns = [0x7F81, 0x7FBF, -0x007F] if kind == "bf16" else [0x7F800001, 0x7FBFFFFF, -0x007FFFFF]
+    for i, at in enumerate((63, 67, 68, 71, 72, 131, vocab - 1)):
+        bits[0, at] = patterns[i % 3]
+    bits[1, 4] = patterns[0]
+    got = ra.token_logprobs(x, tokens_of(tokens), top=9)
+    want = ends.token_logprobs(H.f64(x[:3]), tokens[:3], None, 9)
+    assert np.array_equal(got.top_ids[:3].cpu().numpy(), want["top_ids"])
+    assert torch.isnan(got.logprobs[:2]).all() and torch.isfinite(got.logprobs[2:]).all()
+    ra.check_device_errors()
+
+
+@pytest.mark.parametrize("vocab", [9001, 270001])
+def test_alternatives_of_many_rows(vocab):
+    """A workgroup to a row, of few and of many segments, gives what the workgroups that share a row give."""
+    x, tokens, _ = make(15, 2100, vocab, "bf16")
+    t = tokens_of(tokens)
+    many = ra.token_logprobs(x, t, top=20)
+    for lo in (0, 1000, 2093):
+        few = ra.token_logprobs(x[lo:lo + 7], t[lo:lo + 7], top=20)
+        assert torch.equal(few.top_ids, many.top_ids[lo:lo + 7])
+        assert torch.equal(few.top_logprobs, many.top_logprobs[lo:lo + 7])
+    check(few, x[2093:], tokens[2093:], None, 20)
