@@ -4,7 +4,7 @@
 //   d_x = r (u - n mean(u n)),  d_w = sum over rows and heads of g n.
 //
 // A pass over two rows in and one out, HBM-bound at 3 x 256 bytes a head row, beside
-// some 350 VALU instructions for eight of them (half of its time). A wave takes eight
+// some 350 VALU instructions for eight of them (46% busy). A wave takes eight
 // head rows of a row at a time and loads the next ones before it uses these, a
 // workgroup rows of q or of k only, and its sums of the weights' gradients stay in
 // registers until it is through; they are added up in one order by a second launch, so
