@@ -22,8 +22,8 @@
 // TB/s (4096 rows of 131072 bf16 logits, a third left out, 118 us; a large copy runs
 // at 4.9, a read at 7.2). Rows that would not fill the device are shared by up to 16
 // workgroups, the last of which to arrive answers (two launches took 3-4 us more): 128
-// rows of 131072 take 12.6 us, with 20 alternatives 17.8 (38 with a first form that
-// counted larger maxima thread by thread), one row of 32000 6.1 and 10.6, a chain of
+// rows of 131072 take 12.6 us, with 20 alternatives 17.1 (38 with a first form that
+// counted larger maxima thread by thread), one row of 32000 6.1 and 10.5, a chain of
 // dependent steps of about 1 us. The gradient is a copy with an exponential: 5.7 TB/s.
 #include <algorithm>
 
@@ -267,35 +267,71 @@ struct TopLds {
   __attribute__((aligned(16))) uint64_t cand[kCand];
   uint64_t best[kLogprobTop];
   uint32_t tau;
-  union {
+  union __attribute__((aligned(16))) {
     int winners[kCand];                             // rounds << 8 | threads whose logits are read again
     uint64_t mine[kLpWaves][kHeldCand];             // of each wave
   };
   int n_winners, n_cand;
 };
 
-// The `top` largest of t.cand[0 .. n) to t.best, in order; 0 behind the last. (Each
-// counts the larger ones; reads of a fixed number at a time overlap.)
-__device__ __forceinline__ void rank_candidates(TopLds& t, int n, int top) {
+// The `top` largest of list[0 .. n) to t.best, in order; 0 behind the last. (Each
+// counts the larger ones; reads of a fixed number at a time overlap. The list has room
+// for a multiple of sixteen.)
+__device__ __forceinline__ void rank_candidates(TopLds& t, uint64_t* list, int n, int top) {
   typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
   const int tid = threadIdx.x;
-  const int padded = (n + 15) & ~15;                // (kCand is a multiple of 16)
+  const int padded = (n + 15) & ~15;
   if (tid < top) t.best[tid] = 0;
-  if (tid < padded - n) t.cand[n + tid] = 0;
+  if (tid < padded - n) list[n + tid] = 0;
   __syncthreads();
   for (int i = tid; i < n; i += kLpThreads) {
-    const uint64_t mine = t.cand[i];
+    const uint64_t mine = list[i];
     int rank = 0;
     for (int j = 0; j < padded; j += 16) {
 #pragma unroll
       for (int k = 0; k < 16; k += 2) {
-        const u64x2 two = *reinterpret_cast<const u64x2*>(&t.cand[j + k]);
+        const u64x2 two = *reinterpret_cast<const u64x2*>(&list[j + k]);
         rank += (two.x > mine) + (two.y > mine);
       }
     }
     if (mine != 0 && rank < top) t.best[rank] = mine;
   }
   __syncthreads();
+}
+
+// The same of `chunks` lists of `top` in order, in t.cand: each has top / chunks, rounded
+// up, entries that reach the least of those entries, so only what reaches it is ranked,
+// some 40 of 160 (128 rows of 131072, 20 alternatives 18.6 -> 18.1 us, 32 of them 20.9 ->
+// 18.8; lists of fewer than 96 entries in all would take 0.3 longer than ranking them).
+__device__ __forceinline__ void rank_lists(TopLds& t, int chunks, int top) {
+  const int tid = threadIdx.x, lane = tid & 63, n = chunks * top, each = (top + chunks - 1) / chunks;
+  if (n < 96) {
+    rank_candidates(t, t.cand, n, top);
+    return;
+  }
+  uint64_t* some = &t.mine[0][0];
+  if (tid == 0) t.n_cand = 0;
+  uint64_t bound = ~0ull;
+#pragma unroll 4
+  for (int c = 0; c < chunks; ++c) bound = min(bound, t.cand[c * top + each - 1]);
+  __syncthreads();
+  for (int i0 = 0; i0 < n; i0 += kLpThreads) {
+    const int i = i0 + tid;
+    const uint64_t v = i < n ? t.cand[i] : 0;
+    const bool in = v != 0 && v >= bound;
+    const uint64_t m = __builtin_amdgcn_ballot_w64(in);
+    int at = 0;
+    if (lane == 0 && m != 0) at = atomicAdd(&t.n_cand, __popcll(m));
+    at = __builtin_amdgcn_readfirstlane(at) +
+         __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
+    if (in && at < kLpWaves * kHeldCand) some[at] = v;
+  }
+  __syncthreads();
+  const int found = t.n_cand;
+  if (found <= kLpWaves * kHeldCand)
+    rank_candidates(t, some, found, top);
+  else
+    rank_candidates(t, t.cand, n, top);
 }
 
 // A bound that at least `top` of the workgroup's threads' largest logits reach, and
@@ -307,8 +343,18 @@ __device__ __forceinline__ void find_bound(TopLds& t, float lane_max, int top) {
   __syncthreads();
   if (tid < 64) {
     const u32x4 w = *reinterpret_cast<const u32x4*>(&t.keys[4 * tid]);
-    uint32_t lo = 0;
-    for (int shift = 30; shift >= 0; shift -= 2) {
+    // from the highest pair of bits in which they differ
+    uint32_t all = w[0] & w[1] & w[2] & w[3], some = w[0] | w[1] | w[2] | w[3];
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      all &= __shfl_xor(all, m);
+      some |= __shfl_xor(some, m);
+    }
+    all = __builtin_amdgcn_readfirstlane(all);
+    some = __builtin_amdgcn_readfirstlane(some);
+    const int from = all == some ? 0 : (31 - __builtin_clz(all ^ some)) & ~1;
+    uint32_t lo = some & ~((4u << from) - 1);       // (the shared bits; 4 << 30 is 0)
+    for (int shift = from; shift >= 0; shift -= 2) {
       int n[4];                                     // threads that reach lo + k steps
 #pragma unroll
       for (int k = 1; k < 4; ++k) {
@@ -424,7 +470,7 @@ __device__ __forceinline__ void find_top(TopLds& t, const X* x, int vocab, int s
   __syncthreads();
   int found = t.n_cand;
   if (found <= kCand) {
-    rank_candidates(t, found, top);
+    rank_candidates(t, t.cand, found, top);
     return;
   }
   // odd values, or so many equal logits that the list does not hold them: one after the
@@ -533,7 +579,7 @@ __global__ __launch_bounds__(kLpThreads, kLpWavesPerSimd) void logprob_kernel(Lo
       if (wave != 0)
         for (int i = tid - 64; i < n; i += kLpThreads - 64) top.cand[i] = handed_over(cands + i);
       __syncthreads();
-      rank_candidates(top, n, a.top);
+      rank_lists(top, a.chunks, a.top);
     }
   } else {
     __syncthreads();
