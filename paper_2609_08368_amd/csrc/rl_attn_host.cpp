@@ -322,8 +322,9 @@ int acquire_ws(hipStream_t st, size_t need, size_t want, bool need_stash, Worksp
     e = hipMalloc(&p, kErrBlockBytes);
     if (e != hipSuccess)
       return fail(RL_ERR_WORKSPACE, "hipMalloc(%zu) for the error word failed: %s", kErrBlockBytes, hipGetErrorString(e));
-    e = hipMemset(p, 0, kErrBlockBytes);
-    if (e != hipSuccess) return hip_fail(e, "hipMemset");
+    // on the stream itself, whose kernels count on the zeros (it is not being captured here)
+    e = hipMemsetAsync(p, 0, kErrBlockBytes, st);
+    if (e != hipSuccess) return hip_fail(e, "hipMemsetAsync");
     w.err = static_cast<int*>(p);
   }
   if (grow) {
