@@ -15,6 +15,7 @@
 // The copies are HBM-bound behind their ramp: 128 times 32 rows of 8 heads, K and V, 6.0
 // us, 5.6 TB/s.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_common.hpp"
 #include "kernels.hpp"
@@ -241,13 +242,21 @@ __device__ __forceinline__ int list_pages(const DropArgs& a, const uint64_t* mar
   }
   __syncthreads();
   const int start = end - total;
+  const unsigned bit = 1u << (lane & 31);
+  // (the list is mostly dense: without a 64-bit product an id)
+  auto list = [&](auto stride) {
 #pragma unroll 4
-  for (int i = tid >> 6; i < n; i += kDropWaves) {
-    const uint64_t x = marks[i];
-    const int below = __builtin_amdgcn_mbcnt_hi((unsigned)(x >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)x, 0));
-    const int to = start + base[i] + below;
-    if ((x >> lane & 1) && to >= 0) a.free_pages[(int64_t)to * a.free_s] = first + 64 * i + lane;
-  }
+    for (int i = tid >> 6; i < n; i += kDropWaves) {
+      const uint64_t x = marks[i];
+      const unsigned lo = (unsigned)x, hi = (unsigned)(x >> 32);
+      const int to = start + base[i] + __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+      if (((lane < 32 ? lo : hi) & bit) && to >= 0) a.free_pages[to * stride] = first + 64 * i + lane;
+    }
+  };
+  if (a.free_s == 1)
+    list(std::integral_constant<int, 1>{});
+  else
+    list(a.free_s);
   return total;
 }
 
