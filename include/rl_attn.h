@@ -403,7 +403,8 @@ size_t rl_attn_norm_rope_backward_workspace_size(void);
  *              likeliest tokens, larger logits first, of equal ones the lower index;
  *              -1 and -inf where fewer than K tokens have a logit above -inf
  * Logits of -inf exclude tokens (log probability -inf); a row of nothing else has
- * lse = logprob = -inf and entropy 0. A row with a NaN or +inf gives NaN, and its
+ * lse = logprob = -inf and entropy 0. A row with a NaN or +inf gives NaN
+ * (one whose largest scaled logit passes 2^126 in magnitude may), and its
  * alternatives are those among the others and +inf. A row's bits
  * depend on its own logits, token and scale alone: not on the other rows of the
  * call, its size, or where the row lies (section "True-On-Policy Alignment" asks
@@ -421,7 +422,8 @@ size_t rl_attn_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int64_
  *              wrote them (entropy is read only with d_entropy)
  *   d_logprobs, d_entropy [T] f32, any stride from 0 on; one may be NULL (0)
  *   d_logits   [T, V] of the logits' type, written; may be logits (the same view)
- * Rows that are left out, or without a token above -inf, get zeros. */
+ * Rows that are left out, or without a token above -inf, get zeros; a row whose lse is
+ * NaN gets NaN. */
 int rl_attn_token_logprobs_backward(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale,
                                     const rl_tensor* lse, const rl_tensor* entropy, const rl_tensor* d_logprobs,
                                     const rl_tensor* d_entropy, rl_tensor* d_logits, void* stream);
