@@ -423,7 +423,9 @@ size_t rl_attn_token_logprobs_workspace_size(int64_t rows, int64_t vocab, int64_
  *   d_logprobs, d_entropy [T] f32, any stride from 0 on; one may be NULL (0)
  *   d_logits   [T, V] of the logits' type, written; may be logits (the same view)
  * Rows that are left out, or without a token above -inf, get zeros; a row whose lse is
- * NaN gets NaN. */
+ * NaN gets NaN. p is formed from lse where that is at most 64 in magnitude; the powers of
+ * rows farther out, whose lse is rounded too much, are summed again by one workgroup each
+ * (twice the time for thousands of rows, up to twelve times for a hundred). */
 int rl_attn_token_logprobs_backward(const rl_tensor* logits, const rl_tensor* tokens, const rl_tensor* row_scale,
                                     const rl_tensor* lse, const rl_tensor* entropy, const rl_tensor* d_logprobs,
                                     const rl_tensor* d_entropy, rl_tensor* d_logits, void* stream);

@@ -591,8 +591,78 @@ __global__ __launch_bounds__(kLpThreads, kLpWavesPerSimd) void logprob_kernel(Lo
   }
 }
 
-// Gradient: d_x_j = s (g (delta_j - p_j) - h p_j (ln p_j + H)), an element-wise pass.
+// Gradient: d_x_j = s (g (delta_j - p_j) - h p_j (ln p_j + H)), an element-wise pass with
+// ln p_j = s x_j - lse. That lse is rounded, so p is off by half a step of it, relatively:
+// 2^-19 below kLseNear, no more than the products and powers of a token with |ln p| = 10
+// are off by, but 3e-5 at 1000 and everything at 1e7. Rows past kLseNear are therefore one
+// workgroup's, which sums their powers again, around their largest logit m, and takes
+// ln p_j = (x_j - m) s + rest as the forward call does; behind the row's last load, as the
+// row may be in place. They cost a second read, 4096 rows of 131072 bf16 logits 702 us
+// (343 with lse in every workgroup), and calls of few rows are as slow as one workgroup:
+// 128 rows 158 us (13; 71 of 151936 logits, whose rows do not all begin on one channel).
 constexpr int kGradLoads = 4;
+constexpr float kLseNear = 64.f;
+
+// A row's largest logit and -ln of the sum of exp((x_j - m) scale), by a workgroup: one
+// read of the row. A thread's sum is taken around one of its logits, another one only
+// when a logit is 2^kAhead times as likely, so that what is rounded then fades.
+template <typename X>
+__device__ __forceinline__ void sum_again(const X* x, int vocab, float scale, float* m_out, float* rest_out) {
+  __shared__ float most[kLpWaves], sums[kLpWaves];
+  constexpr float kAhead = 8.f;
+  const int tid = threadIdx.x;
+  const float c = scale * kLog2e;
+  float base = kNegInf;
+  double sum = 0.0;                                 // (of up to 2^21 / 256 logits)
+  for (int e0 = tid * kPer<X>; e0 < vocab; e0 += kGradLoads * kLpThreads * kPer<X>) {
+    u32x4 w[kGradLoads];
+#pragma unroll
+    for (int i = 0; i < kGradLoads; ++i) w[i] = load_logits(x, e0 + i * kLpThreads * kPer<X>, vocab);
+    float top = kNegInf;
+#pragma unroll
+    for (int i = 0; i < kGradLoads; ++i) {
+      float f[kPer<X>];
+      unpack<X>(w[i], f);
+#pragma unroll
+      for (int j = 0; j < kPer<X>; ++j) top = fmaxf(top, f[j]);
+    }
+    if (top == kNegInf && base == kNegInf) continue;                      // (excluded tokens alone)
+    if (base == kNegInf) base = top;
+    if ((top - base) * c > kAhead) {
+      sum *= (double)exp2_fast((base - top) * c);
+      base = top;
+    }
+#pragma unroll
+    for (int i = 0; i < kGradLoads; ++i) {
+      float f[kPer<X>], t = 0.f;
+      unpack<X>(w[i], f);
+#pragma unroll
+      for (int j = 0; j < kPer<X>; ++j) t += exp2_fast((f[j] - base) * c);
+      sum += (double)t;
+    }
+  }
+  const float wave_top = wave_max(base);
+  if ((tid & 63) == 0) most[tid >> 6] = wave_top;
+  __syncthreads();
+  float m = most[0];
+#pragma unroll
+  for (int i = 1; i < kLpWaves; ++i) m = fmaxf(m, most[i]);
+  const float mine = wave_sum(base == kNegInf ? 0.f : (float)sum * exp2_fast((base - m) * c));
+  if ((tid & 63) == 0) sums[tid >> 6] = mine;
+  __syncthreads();
+  float all = 0.f;
+#pragma unroll
+  for (int i = 0; i < kLpWaves; ++i) all += sums[i];
+  *m_out = m;
+  *rest_out = -kLn2 * __builtin_amdgcn_logf(all);
+}
+
+// The workgroup of a row that has all of it: workgroups go to the eight dies in turn, and
+// these should too, whatever number of them a row has.
+__device__ __forceinline__ int far_chunk(int row, int chunks) {
+  const int even = chunks % 8 == 0 ? 8 : chunks % 4 == 0 ? 4 : chunks % 2 == 0 ? 2 : 1;
+  return (int)((int64_t)row * even / 8 % chunks);
+}
 
 template <typename X>
 __global__ __launch_bounds__(kLpThreads) void logprob_grad_kernel(LogprobArgs a) {
@@ -624,27 +694,38 @@ __global__ __launch_bounds__(kLpThreads) void logprob_grad_kernel(LogprobArgs a)
     }
     return;
   }
-  u32x4 w[kGradLoads];
+  // the gradient of the logits from element e on, with ln p = (x - m) s + rest
+  auto pass = [&](int e0, float m, float rest) {
+    u32x4 w[kGradLoads];
 #pragma unroll
-  for (int i = 0; i < kGradLoads; ++i) w[i] = load_logits(x, e0 + i * kLpThreads * kPer<X>, a.vocab);
+    for (int i = 0; i < kGradLoads; ++i) w[i] = load_logits(x, e0 + i * kLpThreads * kPer<X>, a.vocab);
 #pragma unroll
-  for (int i = 0; i < kGradLoads; ++i) {
-    const int e = e0 + i * kLpThreads * kPer<X>;
-    float f[kPer<X>];
-    unpack<X>(w[i], f);
+    for (int i = 0; i < kGradLoads; ++i) {
+      const int e = e0 + i * kLpThreads * kPer<X>;
+      float f[kPer<X>];
+      unpack<X>(w[i], f);
 #pragma unroll
-    for (int j = 0; j < kPer<X>; ++j) {
-      const float lp = fmaf(f[j], in.scale, -lse), p = exp2_fast(lp * kLog2e);
-      const float v = -p * fmaf(h, fmaxf(lp, -1000.f) + ent, g);          // (0 times -inf)
-      f[j] = in.scale * (e + j == in.token ? v + g : v);
+      for (int j = 0; j < kPer<X>; ++j) {
+        const float lp = fmaf(f[j] - m, in.scale, rest), p = exp2_fast(lp * kLog2e);
+        const float v = -p * fmaf(h, fmaxf(lp, -1000.f) + ent, g);        // (0 times -inf)
+        f[j] = in.scale * (e + j == in.token ? v + g : v);
+      }
+      if (e + kPer<X> <= a.vocab)
+        __builtin_nontemporal_store(pack<X>(f), reinterpret_cast<u32x4_any*>(d + e));
+      else
+#pragma unroll
+        for (int j = 0; j < kPer<X>; ++j)
+          if (e + j < a.vocab) d[e + j] = (X)f[j];
     }
-    if (e + kPer<X> <= a.vocab)
-      __builtin_nontemporal_store(pack<X>(f), reinterpret_cast<u32x4_any*>(d + e));
-    else
-#pragma unroll
-      for (int j = 0; j < kPer<X>; ++j)
-        if (e + j < a.vocab) d[e + j] = (X)f[j];
+  };
+  if (fabsf(lse) <= kLseNear) {
+    pass(e0, 0.f, -lse);
+    return;
   }
+  if (chunk != far_chunk(row32, a.chunks)) return;
+  float m, rest;
+  sum_again(x, a.vocab, in.scale, &m, &rest);
+  for (int e = threadIdx.x * kPer<X>; e < a.vocab; e += kGradLoads * kLpThreads * kPer<X>) pass(e, m, rest);
 }
 
 }  // namespace
