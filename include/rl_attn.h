@@ -404,8 +404,10 @@ size_t rl_attn_norm_rope_backward_workspace_size(void);
  *              -1 and -inf where fewer than K tokens have a logit above -inf
  * Logits of -inf exclude tokens (log probability -inf); a row of nothing else has
  * lse = logprob = -inf and entropy 0. A row with a NaN or +inf gives NaN
- * (one whose largest scaled logit passes 2^126 in magnitude may), and its
- * alternatives are those among the others and +inf. A row's bits
+ * (one whose scale or largest scaled logit passes 2^126 in magnitude may), and its
+ * alternatives are those among the others and +inf. Log probabilities and entropies
+ * near 0 (a sure token's) are off by some 1e-7 whatever their size, as a log softmax in
+ * 32 bits is: they come from a sum next to 1. A row's bits
  * depend on its own logits, token and scale alone: not on the other rows of the
  * call, its size, or where the row lies (section "True-On-Policy Alignment" asks
  * for batch invariance). Calls of fewer rows than 8 a compute unit need

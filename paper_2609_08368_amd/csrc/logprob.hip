@@ -10,7 +10,12 @@
 // made them, so that a row's bits depend on its logits alone: not on the size of
 // the call, on how its rows are shared out or on where they lie.
 //   lse = s M + ln 2 log2 S,  entropy = ln 2 (log2 S - Y / S)
-// (all terms of one size, none cancelled: Y is taken around the maximum).
+// Y is taken around a base within half a power of two of the maximum, so neither term is
+// larger than 1/2 or the entropy. The entropy of a sure row is what is left of the two,
+// and of a sum next to 1: off by 1e-7 on average and 4e-7 at most over 1024 rows with
+// entropies from 1e-6 to 4e-3. (With y = (x - m) c, so that the maximum adds 1 and 0, by
+// 1e-7 and 2.3e-6, as small powers added to 1 one by one all round the same way, and
+// 6e-7 with those added in pairs; both took 2-5% longer.)
 //
 // Alternatives: a bound that K of a workgroup's threads' largest logits reach bounds
 // the K-th largest logit from below, so only those threads hold any of the K
