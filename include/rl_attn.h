@@ -468,7 +468,8 @@ int rl_attn_fork_requests(const rl_tensor* parents, const rl_tensor* fork_lens, 
  *              scale serves all pages of a head)
  * A page outside the pool, or more rows than a page has, is reported and not
  * copied. Pages that are copied to must differ from each other and from those
- * copied from. */
+ * copied from. Pools whose rows overlap themselves, each other in part, or copies are
+ * refused (slices of one buffer with the same strides that share no byte are taken). */
 int rl_attn_copy_pages(const rl_tensor* copies, rl_tensor* k_pages, rl_tensor* v_pages, void* stream);
 
 /* Requests that end, or are cut back to an earlier token (a turn tried again,

@@ -200,6 +200,54 @@ bool runs_meet(Runs a, Runs b, bool self) {
   return false;
 }
 
+// The bytes of a pool [pages, P, heads, 128]: n2 views s2 bytes apart. Dimensions that lie side by side are one run or
+// one dimension, so mostly n2 is 1.
+struct PoolRuns {
+  Runs r;
+  int64_t n2, s2;
+};
+PoolRuns pool_of(const Runs& r) { return {r, 1, 0}; }
+PoolRuns pool_of(const rl_tensor* t) {
+  struct Dim {
+    int64_t n, s;
+  };
+  const int64_t e = elem_bytes(t->dtype);
+  Dim d[4];
+  int n = 0;
+  for (int i = 0; i < 3; ++i)
+    if (t->shape[i] != 1) d[n++] = {t->shape[i], e * t->strides[i]};
+  std::sort(d, d + n, [](const Dim& a, const Dim& b) { return a.s < b.s; });
+  int64_t width = e * t->shape[3];
+  int first = 0, m = 0;
+  for (; first < n && d[first].s == width; ++first) width *= d[first].n;
+  for (int i = first; i < n; ++i) {
+    if (m > 0 && d[i].s == d[m - 1].n * d[m - 1].s)
+      d[m - 1].n *= d[i].n;
+    else
+      d[m++] = d[i];
+  }
+  for (int i = m; i < 3; ++i) d[i] = {1, 0};
+  if (width == 0) d[0].n = 0;                       // (an empty dimension was taken into the run)
+  return {{reinterpret_cast<intptr_t>(t->data), d[1].n, d[1].s, d[0].n, d[0].s, width}, d[2].n, d[2].s};
+}
+// As runs_meet.
+bool pools_meet(PoolRuns a, PoolRuns b, bool self) {
+  if (a.n2 < 1 || b.n2 < 1 || a.r.n0 < 1 || a.r.n1 < 1 || b.r.n0 < 1 || b.r.n1 < 1) return false;
+  auto end = [](const PoolRuns& p) {
+    return p.r.at + (p.r.n0 - 1) * p.r.s0 + (p.r.n1 - 1) * p.r.s1 + (p.n2 - 1) * p.s2 + p.r.width;
+  };
+  if (a.r.at >= end(b) || b.r.at >= end(a)) return false;
+  if (a.n2 == 1) a.s2 = b.s2;
+  if (b.n2 == 1) b.s2 = a.s2;
+  if (a.s2 != b.s2) return true;
+  for (int64_t d2 = 1 - b.n2; d2 < a.n2; ++d2) {
+    Runs x = a.r;
+    x.at += d2 * a.s2;
+    if (runs_meet(x, b.r, self && d2 == 0)) return true;
+  }
+  return false;
+}
+
 struct Named {
   const rl_tensor* t;
   const char* name;
@@ -1758,6 +1806,17 @@ int copy_pages_impl(const rl_tensor* copies, rl_tensor* k_pages, rl_tensor* v_pa
   // (a launch has fewer than 2^32 threads, 512 for 16 KB of a page)
   if (n * ((P * Hkv * 128 * e + 16383) / 16384) >= (1 << 23)) return fail(RL_ERR_UNSUPPORTED, "copies too many");
   if (n == 0 || Hkv == 0) return RL_OK;
+  const PoolRuns k = pool_of(k_pages), v = pool_of(v_pages), c = pool_of(runs_of(copies));
+  for (const auto& t : {std::make_pair(&k, "k_pages"), std::make_pair(&v, "v_pages")}) {
+    if (pools_meet(*t.first, *t.first, true))
+      return fail(RL_ERR_UNSUPPORTED, "%s: elements that are written must not overlap", t.second);
+    if (pools_meet(*t.first, c, false)) return fail(RL_ERR_UNSUPPORTED, "%s and copies must not overlap", t.second);
+  }
+  bool same = k_pages->data == v_pages->data;       // (one pool for both is copied twice alike)
+  for (int i = 0; i < 3; ++i)
+    same = same && (k_pages->shape[i] <= 1 || k_pages->strides[i] == v_pages->strides[i]);
+  if (!same && pools_meet(k, v, false))
+    return fail(RL_ERR_UNSUPPORTED, "k_pages must be v_pages or not overlap it");
   hipStream_t st = static_cast<hipStream_t>(stream);
   Workspace* w = nullptr;
   RL_TRY(acquire_ws(st, 0, 0, false, &w));          // the error word only
