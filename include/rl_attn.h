@@ -261,8 +261,9 @@ int rl_attn_append_kv_fp8(const rl_tensor* k_new, const rl_tensor* v_new, const 
  * is said, as the same view; otherwise no output may overlap itself, another
  * output or an input. Lengths, tables, rows and log-sum-exps that do are refused
  * (views of one buffer that share no byte are apart if they have the same
- * strides); that pages, positions and slots are apart from them is the
- * caller's part. */
+ * strides), and rows written into the pages of the same call; that positions and
+ * slots are apart from what is written, and the pages from what is read and from
+ * each other, is the caller's part. */
 
 /* Slot maps (paper: every turn appends its suffix to cached context, section
  * "Fast Agentic Rollout with SGLang"): from the lengths of a step's requests,

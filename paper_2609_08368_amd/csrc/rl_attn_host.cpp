@@ -1397,6 +1397,15 @@ int rope_impl(const rl_tensor* q, const rl_tensor* k, const rl_tensor* v, const 
                         {norm ? norm->q_weight : nullptr, "q_weight"}, {norm ? norm->k_weight : nullptr, "k_weight"}};
   const rl_tensor* same[] = {q, k};
   RL_TRY(check_apart(outs, same, 2, ins, 5));
+  if (append) {                                     // (rows that are written, and pages that are)
+    const Named pools[] = {{k_pages, "k_pages"}, {v_pages, "v_pages"}};
+    for (const Named& p : pools) {
+      const PoolRuns x = pool_of(p.t);
+      for (const Named& o : outs)
+        if (o.t && pools_meet(pool_of(runs_of(o.t)), x, false))
+          return fail(RL_ERR_UNSUPPORTED, "%s and %s must not overlap", o.name, p.name);
+    }
+  }
   int cus = 0;
   RL_TRY(current_cus(&cus));
   hipStream_t st = static_cast<hipStream_t>(stream);

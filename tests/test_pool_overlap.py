@@ -1,5 +1,5 @@
-"""Page copies refuse pools whose rows overlap, before anything is launched; slices of one buffer that share no byte are
-taken, and copied right."""
+"""Page copies refuse pools whose rows overlap, and calls that append refuse rows that are written into the pages they write,
+before anything is launched; slices of one buffer that share no byte are taken, and copied right."""
 
 import numpy as np
 import pytest
@@ -7,8 +7,8 @@ import torch
 
 from paper_2609_08368_amd import rl_attn as ra
 from tests.test_abi import FAKE, fake
-from tests.test_ends_abi import refusals
-from tests.test_step_abi import BF16, FP8, I32
+from tests.test_ends_abi import EPS, refusals
+from tests.test_step_abi import BF16, FP8, I32, append_args, refused
 
 ROWS = 128 * 2                   # bytes of a head row
 POOL = 9 * 16 * 2 * ROWS         # of a dense pool
@@ -46,6 +46,28 @@ def test_copy_of_nothing_in_pools_of_no_pages():
     call = lambda **kw: ra.lib().rl_attn_copy_pages(*(ra.ctypes.byref(t) for t in copy_args(**kw).values()), None)
     assert call(c=fake([0, 3], I32), v=fake(SHAPE, BF16)) == 0
     assert call(k=none(9, 16, 0, 128), v=none(9, 16, 0, 128)) == 0
+
+
+@pytest.mark.parametrize("normed", [False, True])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_append_refuses_rows_in_the_pages(fp8, normed):
+    a = append_args(fp8)
+    if normed:
+        names = list(a)
+        at = names.index("v") + 1
+        w = dict(qw=fake([128], BF16), kw=fake([128], BF16), eps=EPS)
+        a = {k: {**a, **w}[k] for k in names[:at] + list(w) + names[at:]}
+    a["k_out"] = fake([10, 2, 128], BF16)
+    for i, name in enumerate(a):
+        if isinstance(a[name], ra.RlTensor):             # addresses of their own
+            a[name] = fake(list(a[name].shape[:a[name].ndim]), a[name].dtype, FAKE + (i << 24))
+    call = getattr(ra.lib(), f"rl_attn_{'norm_' * normed}rope_append_kv{'_fp8' * fp8}")
+    pool = int(np.prod(a["kp"].shape[:4])) * (1 if fp8 else 2)
+    for name, heads in (("q_out", 8), ("k_out", 2)):
+        for pages in ("kp", "vp"):
+            for at in (0, pool - 16, 16 - 10 * heads * ROWS):
+                refused(call, {**a, name: fake([10, heads, 128], BF16, a[pages].data + at)}, "RL_ERR_UNSUPPORTED",
+                        f"{name} and {pages[0]}_pages must not overlap")
 
 
 def pieces(offset, shape, strides):
