@@ -486,8 +486,10 @@ int rl_attn_copy_pages(const rl_tensor* copies, rl_tensor* k_pages, rl_tensor* v
  *              still taken; may be kv_lens and free_used themselves
  * A page is kept as long as one request holds it within the tokens it keeps, so
  * the tables say which pages are shared; a prefix kept for later requests is a request
- * of its own. A request that is cut back inside a page it shares must be forked there
- * before it grows (its next rows would be written to the others' page). Lengths past
+ * of its own. A request must not be cut back inside a page it shares and then grow: its
+ * next rows would go to the others' page, and nothing reports that. It goes on as another
+ * one: an empty request is forked from it at that length, the rows behind the last full
+ * page are copied (rl_attn_copy_pages), and it ends here, with 0 tokens. Lengths past
  * the table and page ids outside the pool are reported, and such pages not freed; if
  * more pages come back than the list has lost, the ones with the highest ids are
  * written and it is reported. Table entries are left as they are. */
