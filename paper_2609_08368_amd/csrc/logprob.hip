@@ -723,7 +723,10 @@ __global__ __launch_bounds__(kLpThreads) void logprob_grad_kernel(LogprobArgs a)
           if (e + j < a.vocab) d[e + j] = (X)f[j];
     }
   };
-  if (fabsf(lse) <= kLseNear) {
+  // (by bits: a NaN is near, as lse carries it to the whole row and sums that skip
+  // stretches of nothing else would not)
+  const uint32_t size = __float_as_uint(lse) & 0x7fffffffu;
+  if (size <= __builtin_bit_cast(uint32_t, kLseNear) || size > 0x7f800000u) {
     pass(e0, 0.f, -lse);
     return;
   }

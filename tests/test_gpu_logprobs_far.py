@@ -164,3 +164,19 @@ def test_gradient_of_far_rows_captured_and_replayed():
             graph.replay()
             s.synchronize()
             assert torch.equal(d, want)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_gradient_of_rows_with_nan_anywhere(kind):
+    """NaN at one place, in whole stretches of the row, beside excluded tokens: the whole row, whatever its other logits are."""
+    x, tokens, rng = make(21, 12, 30011, kind)
+    x[::2] += 1e4
+    nan, inf = float("nan"), float("inf")
+    for i, part in enumerate((slice(7, 8), slice(0, 8192), slice(4096, 20000), slice(30010, None), slice(None))):
+        x[2 * i, part] = nan
+        x[2 * i + 1, part] = nan
+    x[4, 20000:] = -inf
+    x[5, :4096] = -inf
+    x[10, 3] = x[11, 3] = inf
+    d = run(x, tokens, None, np.ones(12), np.ones(12))
+    assert torch.isnan(d).all(dim=1).tolist() == [True] * 12
