@@ -402,7 +402,9 @@ size_t rl_attn_norm_rope_backward_workspace_size(void);
  *   logprobs   [T] f32; entropy, lse [T] f32, nullable
  *   top_ids    [T, K] int32, top_logprobs [T, K] f32, K <= 32, both nullable: the K
  *              likeliest tokens, larger logits first, of equal ones the lower index;
- *              -1 and -inf where fewer than K tokens have a logit above -inf
+ *              -1 and -inf where fewer than K tokens have a logit above -inf. A row
+ *              with hundreds of logits equal to its K-th largest, with a NaN or +inf is
+ *              searched K times over (some ten to a hundred times as long)
  * Logits of -inf exclude tokens (log probability -inf); a row of nothing else has
  * lse = logprob = -inf and entropy 0. A row with a NaN or +inf gives NaN
  * (one whose scale or largest scaled logit passes 2^126 in magnitude may), and its

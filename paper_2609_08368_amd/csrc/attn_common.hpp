@@ -225,7 +225,10 @@ __device__ __forceinline__ uint64_t row_offset(uint32_t pg, uint32_t sp, int slo
 // Data that workgroups hand to the last of them to arrive: stored and loaded by
 // agent-scope atomics, which go through the L2s of the eight dies, so that no
 // workgroup has to write its whole L2 back (a release fence at agent scope in each of
-// 1400 workgroups took a 30 us kernel to 270). arrive() waits for the calling
+// 1400 workgroups took a 30 us kernel to 270). The rule is that nothing else is handed
+// over: the order comes from waiting until those stores are through before the count,
+// not from the language's memory model, so what an ordinary store wrote may still lie in
+// its own die's L2, and an ordinary load may find an old line. arrive() waits for the calling
 // wave's own stores and atomics, then for the workgroup's other waves, and counts; it
 // returns true in every thread of the last of n workgroups, which leaves the counter
 // at 0. All threads call it.

@@ -21,7 +21,10 @@
 // the K-th largest logit from below, so only those threads hold any of the K
 // likeliest. Their logits are looked at again (in registers, or read again, and then
 // only those of the segments whose largest reaches the bound), and the few that reach
-// the bound are ranked.
+// the bound are ranked. A row of which more than kCand logits reach it (equal ones, most
+// of all a constant row) or that has a NaN or +inf is searched K times instead, a pass over a
+// workgroup's segments for each: 128 constant rows of 131072 with 20 alternatives take 250
+// us (19 otherwise), 2048 of them 7.5 ms (0.1).
 //
 // A row of a large call is one workgroup's: one pass over the logits, HBM-bound at 6.3
 // TB/s (4096 rows of 131072 bf16 logits, a third left out, 118 us; a large copy runs

@@ -12,8 +12,8 @@
 //
 // The bytes are few; both are chains of dependent loads on top of a launch: 128 forks
 // take 6.2 us, drops of 128 requests with 44K table entries 14, of 3000 with 86K 20.5.
-// The copies are HBM-bound behind their ramp: 128 times 32 rows of 8 heads, K and V, 6.0
-// us, 5.6 TB/s.
+// The copies are bound by their launch and ramp: 128 times 32 rows of 8 heads, K and V,
+// 6.0 us for 16.8 MB written and 2.1 MB read (eight requests copy one page), 3.1 TB/s.
 #include <algorithm>
 #include <type_traits>
 
